@@ -51,8 +51,9 @@ typedef enum {
   ELITEKV_ERR_TIMEOUT = -5,       /* a bounded device-side wait ran out            */
   ELITEKV_ERR_BAD_PAGE = -6,      /* page id outside [0, num_pages)                */
   ELITEKV_ERR_BAD_POSITION = -7,  /* position outside [0, max_pos) or the cache    */
-  ELITEKV_ERR_STATIC_SCRATCH_EXCEEDED = -8  /* elitekv_decode_static: batch/shape needs more
+  ELITEKV_ERR_STATIC_SCRATCH_EXCEEDED = -8, /* elitekv_decode_static: batch/shape needs more
                                                scratch than ELITEKV_STATIC_SCRATCH_BYTES     */
+  ELITEKV_ERR_NO_PAGES = -9       /* elitekv_step_tables: fewer free pages than the step needs */
 } elitekv_status;
 
 /* Layer description (Sections 3.1 and 3.2).  Host struct; elite_idx is a HOST pointer, the
@@ -212,6 +213,101 @@ int elitekv_attend_rows_workspace_size(const elitekv_layer* layer, int32_t B, in
 int elitekv_attend_rows(const elitekv_layer* layer, const elitekv_cache* cache, const void* q_rope,
                         const void* q_abs, const int32_t* seq_lens, int32_t B, int32_t m,
                         void* workspace, size_t workspace_bytes, void* out, elitekv_stream_t stream);
+
+/* ---- Speculative decoding with a tree of drafted tokens ----------------------------------------
+ * A step of a serving loop, sequence b holding held[b] committed tokens and fresh[b] <= m drafts:
+ *   elitekv_step_tables   pages, slots, rotary positions and masks of the step, from the lengths
+ *   elitekv_append_slots  the drafts' cache rows (siblings share a position, never a slot)
+ *   elitekv_absorb_query  on the B*m rows, q_pos = pos
+ *   elitekv_attend_tree   attention of every node over the committed tokens and its ancestors
+ *   elitekv_accept_tree   the branch that the model confirms joins the committed tokens
+ * Node i of sequence b is cached at position held[b] + i; its parent is a node before it, or -1 for
+ * the committed tokens (an entry that is not a node before i counts as -1).  The paper has no
+ * counterpart of the tables and the acceptance; the attention is the score equation of Section 3.1
+ * for several queries with the tree in place of the causal rule.  Serving only: no gradients. */
+#define ELITEKV_MAX_TREE_NODES 64
+#define ELITEKV_MAX_TABLE_SEQS 8192
+
+/* Inputs and outputs of elitekv_step_tables.  Host struct, DEVICE pointers; outputs overlap no
+ * input, except that page_table is updated in place (entries of pages already held are not written). */
+typedef struct {
+  /* in */
+  const int32_t* held;         /* [B] tokens in the cache                                             */
+  const int32_t* fresh;        /* [B] new tokens (m > 0: at most m)                                   */
+  const int32_t* parent;       /* [B][m], or NULL: a chain                                            */
+  const int32_t* pages_held;   /* [B] valid entries of the sequence's row of the page table, at least
+                                  ceil(held / page_size)                                              */
+  const int32_t* free_pages;   /* [n_free] stack of free page ids, its top at the end                 */
+  const int32_t* n_free;       /* [1]                                                                 */
+  /* out */
+  int32_t* page_table;         /* the cache's own page table                                          */
+  int32_t* pages_held_out;     /* [B]                                                                 */
+  int32_t* n_free_out;         /* [1]: free_pages[0, n_free_out) are free still                       */
+  int32_t* seq_lens;           /* [B] held + fresh                                                    */
+  int32_t* first;              /* [B+1] sums of fresh: token i of sequence b is new token first[b] + i */
+  int32_t* seq_id;             /* [n_slots] sequence, -1: padding                                     */
+  int32_t* pos;                /* [n_slots] rotary position, 0 in padding                             */
+  int64_t* slot;               /* [n_slots] cache row, -1 in padding                                  */
+  uint64_t* tree_mask;         /* [B][m] (m > 0): bit j = node i sees node j; 0 in padding            */
+  int32_t* result;             /* [4]: status, new tokens, pages taken, detail                        */
+} elitekv_tables;
+
+/* Page table, slot map, rotary positions and tree masks of a step from the request lengths, on the
+ * device: no length crosses to the host.
+ *   m == 0   packed: entry first[b] + i is token i of sequence b, at position held[b] + i; entries
+ *            behind the last token, up to n_slots, are padding (a captured step has a fixed size)
+ *   m > 0    trees: n_slots = B*m, entry b*m + i is node i, at position held[b] + its depth
+ * Sequence b needs max(0, ceil((held + fresh) / page_size) - pages_held) more pages; they are taken
+ * from the top of the stack, in order of sequences.  A contiguous cache ignores all page members.
+ * All or nothing: result[0] is ELITEKV_OK, or
+ *   ELITEKV_ERR_NO_PAGES      result[3] pages are missing
+ *   ELITEKV_ERR_BAD_POSITION  sequence result[3]: negative lengths, more tokens than the cache holds, more
+ *                             than m, fewer pages held than tokens; or -1: more tokens than n_slots
+ *   ELITEKV_ERR_BAD_PAGE      result[3]: a page id outside the pool, among those the new tokens go to
+ * and then nothing is granted: the page table is as it was, every entry is padding, seq_lens = held,
+ * first = 0, pages_held_out = pages_held, n_free_out = n_free.
+ * B <= ELITEKV_MAX_TABLE_SEQS, sequences 0 .. B-1 of the cache. */
+int elitekv_step_tables(const elitekv_cache* cache, const elitekv_tables* tables, int32_t B, int32_t m,
+                        int64_t n_slots, elitekv_stream_t stream);
+
+/* elitekv_append with the cache row of every token given (elitekv_step_tables) instead of its
+ * sequence: token t is rotated at pos[t] and written to row slot[t] of the planes; a negative slot is
+ * padding and writes nothing.  A slot outside the planes or a position outside [0, max_pos) is
+ * recorded (BAD_POSITION, detail = token, position) and skipped. */
+int elitekv_append_slots(const elitekv_layer* layer, const elitekv_cache* cache, const void* k_e, const void* c,
+                         const int64_t* slot, const int32_t* pos, int64_t T, elitekv_stream_t stream);
+
+/* Attention of a tree of drafted tokens over the compressed cache:
+ *   s[b,i,h,t] = q_rope[b,i,h] . k_rope[t,h] + q_abs[b,i,h] . c[t]
+ *   o[b,i,h]   = (sum_t softmax_t(scale * s) c[t]) . W_uv,h
+ * over the tokens that node i sees: all committed ones, t < seq_lens[b] - n_nodes[b], and node j's,
+ * t = seq_lens[b] - n_nodes[b] + j, where bit j of tree_mask[b][i] is set.  A row that sees nothing,
+ * and every row i >= n_nodes[b], is a zero row.  Tokens that a row does not see do not touch it,
+ * whatever their cache rows hold.
+ *   q_rope bf16 [B][m][n_h][2r], q_abs bf16 [B][m][n_h][d_c] (separated latents: d_ck), 16-byte aligned
+ *   seq_lens int32 [B] cached tokens, nodes included; n_nodes int32 [B] in [0, m], NULL: m everywhere
+ *   tree_mask uint64 [B][m];   out bf16 [B][m][n_h][d_h], 4-byte aligned
+ *   workspace: 256-byte aligned, elitekv_attend_tree_workspace_size bytes (of shape, B, m and device, not
+ *   of the lengths), private to this call until the stream reaches its end.
+ * 1 <= m <= ELITEKV_MAX_TREE_NODES; any layer and page size.  Results do not depend on scheduling. */
+int elitekv_attend_tree_workspace_size(const elitekv_layer* layer, int32_t B, int32_t m, size_t* bytes);
+int elitekv_attend_tree(const elitekv_layer* layer, const elitekv_cache* cache, const void* q_rope, const void* q_abs,
+                        const int32_t* seq_lens, const int32_t* n_nodes, const uint64_t* tree_mask, int32_t B, int32_t m,
+                        void* workspace, size_t workspace_bytes, void* out, elitekv_stream_t stream);
+
+/* Greedy verification of a tree.  first[b] is the model's choice after the committed tokens, chosen[b][i] the one
+ * after node i.  The accepted branch starts at the lowest node on the committed tokens that drafts first[b]; a node
+ * is followed by its lowest child that drafts what was chosen after it.  Its k-th node's cache row moves, bit for
+ * bit, to position held[b] + k (the position it was rotated at).
+ *   held int32 [B] committed tokens, n_nodes int32 [B] (NULL: m), parent (NULL: a chain), draft, chosen int32 [B][m]
+ *   n_accepted int32 [B]; path int32 [B][m]: the branch, then -1; token int32 [B]: the choice after the branch (the
+ *   next step's `first`); held_out int32 [B] = held + n_accepted.  held_out may be held, token may be first.
+ * Pages beyond the accepted tokens stay with their sequence (elitekv_step_tables uses them first).  A page id outside
+ * the pool is recorded in the layer's status word and the row is not moved. */
+int elitekv_accept_tree(const elitekv_layer* layer, const elitekv_cache* cache, const int32_t* held,
+                        const int32_t* n_nodes, const int32_t* parent, const int32_t* draft, const int32_t* first,
+                        const int32_t* chosen, int32_t B, int32_t m, int32_t* n_accepted, int32_t* path, int32_t* token,
+                        int32_t* held_out, elitekv_stream_t stream);
 
 /* RoPElite search (Algorithm 1, Section 3.1) on calibration activations: which r chunks of every
  * head keep their rotation.  Q, K: bf16 [n_heads][n][d_h], un-rotated queries and keys of a

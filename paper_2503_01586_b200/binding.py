@@ -24,6 +24,8 @@ ERR_TIMEOUT = -5
 ERR_BAD_PAGE = -6
 ERR_BAD_POSITION = -7
 ERR_STATIC_SCRATCH_EXCEEDED = -8
+ERR_NO_PAGES = -9
+MAX_TREE_NODES = 64
 STATIC_SCRATCH_BYTES = 48 << 20
 
 
@@ -48,6 +50,12 @@ class CacheDesc(C.Structure):
                 ("num_pages", C.c_int64), ("max_ctx", C.c_int64), ("n_seqs", C.c_int32)]
 
 
+class TablesDesc(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in
+                ("held", "fresh", "parent", "pages_held", "free_pages", "n_free", "page_table", "pages_held_out", "n_free_out",
+                 "seq_lens", "first", "seq_id", "pos", "slot", "tree_mask", "result")]
+
+
 _lib = None
 
 
@@ -69,6 +77,11 @@ def lib() -> C.CDLL:
         L.elitekv_decode.argtypes = [vp, C.POINTER(CacheDesc), vp, vp, vp, i32, vp, sz, vp, vp]
         L.elitekv_decode_step.argtypes = [vp, C.POINTER(CacheDesc), vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp, vp]
         L.elitekv_copy.argtypes = [vp, vp, i64, vp]
+        L.elitekv_step_tables.argtypes = [C.POINTER(CacheDesc), C.POINTER(TablesDesc), i32, i32, i64, vp]
+        L.elitekv_append_slots.argtypes = [vp, C.POINTER(CacheDesc), vp, vp, vp, vp, i64, vp]
+        L.elitekv_attend_tree_workspace_size.argtypes = [vp, i32, i32, C.POINTER(sz)]
+        L.elitekv_attend_tree.argtypes = [vp, C.POINTER(CacheDesc), vp, vp, vp, vp, vp, i32, i32, vp, sz, vp, vp]
+        L.elitekv_accept_tree.argtypes = [vp, C.POINTER(CacheDesc), vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         L.elitekv_attend_rows_workspace_size.argtypes = [vp, i32, i32, C.POINTER(sz)]
         L.elitekv_attend_rows.argtypes = [vp, C.POINTER(CacheDesc), vp, vp, vp, i32, i32, vp, sz, vp, vp]
         L.elitekv_ropelite_workspace_size.argtypes = [i32, i32, i32, C.POINTER(sz)]
@@ -98,7 +111,8 @@ def lib() -> C.CDLL:
                      "elitekv_project_append", "elitekv_decode_step", "elitekv_copy",
                      "elitekv_attend_rows_workspace_size", "elitekv_attend_rows",
                      "elitekv_ropelite_workspace_size", "elitekv_ropelite_workspace_size_rounds",
-                     "elitekv_ropelite_distances", "elitekv_ropelite_search"):
+                     "elitekv_ropelite_distances", "elitekv_ropelite_search", "elitekv_step_tables", "elitekv_append_slots",
+                     "elitekv_attend_tree_workspace_size", "elitekv_attend_tree", "elitekv_accept_tree"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -276,6 +290,103 @@ def elitekv_attend_rows(layer: Layer, cache: CacheDesc, q_rope, q_abs, seq_lens,
                                      workspace.numel() * workspace.element_size(), _ptr(out), _stream()),
            "elitekv_attend_rows")
     return out
+
+
+class Tables:
+    """Inputs (the caller's tensors) and outputs (made here, or given as `outputs`) of elitekv_step_tables; serves step
+    after step.  result is int32 [4] on the device: status, new tokens, pages taken, detail."""
+
+    def __init__(self, B, n_slots, m, inputs, outputs):
+        self.B, self.n_slots, self.m = B, n_slots, m
+        self._inputs = inputs
+        desc = TablesDesc()
+        for k, v in {**inputs, **outputs}.items():
+            setattr(desc, k, v.data_ptr() if v is not None else None)
+        for k, v in outputs.items():
+            setattr(self, k, v)
+        self.desc = desc
+
+
+def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_table=None, pages_held=None, free_pages=None,
+                n_free=None) -> Tables:
+    """m == 0: packed tokens, up to n_slots; m > 0: trees of up to m nodes, n_slots = B * m.  With a page table (the cache's own)
+    pages_held, free_pages and n_free go with it."""
+    i32, dev = torch.int32, held.device
+    inputs = {"held": held, "fresh": fresh, "parent": parent, "pages_held": pages_held, "free_pages": free_pages, "n_free": n_free}
+    for v in [*inputs.values(), page_table]:
+        if v is not None:
+            _dev(v, i32)
+    if held.numel() < B or fresh.numel() < B:
+        raise ValueError("make_tables: held and fresh have an entry per sequence")
+    if m > 0 and (n_slots != B * m or (parent is not None and parent.numel() < B * m)):
+        raise ValueError("make_tables: trees have B * m slots and parents")
+    if page_table is not None and (pages_held is None or free_pages is None or n_free is None or pages_held.numel() < B):
+        raise ValueError("make_tables: a page table comes with pages_held, free_pages and n_free")
+
+    def empty(*shape, dtype=i32):
+        return torch.empty(shape, dtype=dtype, device=dev)
+    paged = page_table is not None
+    outputs = {"page_table": page_table, "pages_held_out": empty(B) if paged else None, "n_free_out": empty(1) if paged else None,
+               "seq_lens": empty(B), "first": empty(B + 1), "seq_id": empty(n_slots), "pos": empty(n_slots),
+               "slot": empty(n_slots, dtype=torch.int64), "tree_mask": empty(B, m, dtype=torch.int64) if m > 0 else None,
+               "result": empty(4)}
+    return Tables(B, n_slots, m, inputs, outputs)
+
+
+def elitekv_step_tables(cache: CacheDesc, tables: Tables) -> Tables:
+    _check(lib().elitekv_step_tables(C.byref(cache), C.byref(tables.desc), tables.B, tables.m, tables.n_slots, _stream()),
+           "elitekv_step_tables")
+    return tables
+
+
+def elitekv_append_slots(layer: Layer, cache: CacheDesc, k_e, c, slot, pos) -> None:
+    """slot int64 [T] (rows of the planes, negative: padding), pos int32 [T]."""
+    bf16 = torch.bfloat16
+    _check(lib().elitekv_append_slots(layer.handle, C.byref(cache), _ptr(k_e), _in(c, bf16), _in(slot, torch.int64),
+                                      _in(pos, torch.int32), c.shape[0], _stream()), "elitekv_append_slots")
+
+
+def elitekv_attend_tree_workspace_size(layer: Layer, B: int, m: int) -> int:
+    n = C.c_size_t()
+    _check(lib().elitekv_attend_tree_workspace_size(layer.handle, B, m, C.byref(n)), "elitekv_attend_tree_workspace_size")
+    return n.value
+
+
+def elitekv_attend_tree(layer: Layer, cache: CacheDesc, q_rope, q_abs, seq_lens, n_nodes, tree_mask, workspace, out=None):
+    """q_rope [B][m][n_h][2r], q_abs [B][m][n_h][kw], seq_lens and n_nodes (None: m) int32 [B], tree_mask int64 [B][m] (bit j:
+    the node sees node j) -> out [B][m][n_h][d_h]."""
+    B, m = tree_mask.shape
+    bf16, i32 = torch.bfloat16, torch.int32
+    if q_abs.numel() != B * m * layer.n_h * layer.kw:
+        raise ValueError("elitekv_attend_tree: q_abs is [B][m][n_h][kw]")
+    if out is None:
+        out = torch.empty((B, m, layer.n_h, layer.d_h), dtype=bf16, device=q_abs.device)
+    _check(lib().elitekv_attend_tree(layer.handle, C.byref(cache), _ptr(q_rope), _in(q_abs, bf16), _in(seq_lens, i32),
+                                     None if n_nodes is None else _in(n_nodes, i32), _in(tree_mask, torch.int64), B, m,
+                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), _in(out, bf16), _stream()),
+           "elitekv_attend_tree")
+    return out
+
+
+def elitekv_accept_tree(layer: Layer, cache: CacheDesc, held, n_nodes, parent, draft, first, chosen, n_accepted=None, path=None,
+                        token=None, held_out=None):
+    """held, n_nodes (None: m), first int32 [B], parent (None: chain), draft, chosen int32 [B][m].
+    Returns (n_accepted [B], path [B][m], token [B], held_out [B])."""
+    B, m = draft.shape
+    i32 = torch.int32
+    if n_accepted is None:
+        n_accepted = torch.empty(B, dtype=i32, device=draft.device)
+    if path is None:
+        path = torch.empty((B, m), dtype=i32, device=draft.device)
+    if token is None:
+        token = torch.empty(B, dtype=i32, device=draft.device)
+    if held_out is None:
+        held_out = torch.empty(B, dtype=i32, device=draft.device)
+    _check(lib().elitekv_accept_tree(layer.handle, C.byref(cache), _in(held, i32), None if n_nodes is None else _in(n_nodes, i32),
+                                     None if parent is None else _in(parent, i32), _in(draft, i32), _in(first, i32),
+                                     _in(chosen, i32), B, m, _in(n_accepted, i32), _in(path, i32), _in(token, i32),
+                                     _in(held_out, i32), _stream()), "elitekv_accept_tree")
+    return n_accepted, path, token, held_out
 
 
 def elitekv_ropelite_workspace_size(n_heads: int, n: int, d_h: int) -> int:

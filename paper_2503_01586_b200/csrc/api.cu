@@ -114,6 +114,18 @@ extern "C" int elitekv_append(const elitekv_layer* L, const elitekv_cache* cache
   return rc;
 }
 
+extern "C" int elitekv_append_slots(const elitekv_layer* L, const elitekv_cache* cache, const void* k_e, const void* c,
+                                    const int64_t* slot, const int32_t* pos, int64_t T, elitekv_stream_t stream) {
+  if (!L || !cache || T < 0) return ELITEKV_ERR_INVALID_ARG;
+  if (T == 0) return ELITEKV_OK;
+  if (!c || !slot || !pos || (L->r > 0 && !k_e)) return ELITEKV_ERR_INVALID_ARG;
+  if (((uintptr_t)k_e & 15) || ((uintptr_t)c & 15) || ((uintptr_t)slot & 7) || !ekv_on_device(L)) return ELITEKV_ERR_INVALID_ARG;
+  CacheView cv;
+  int rc = ekv_make_view(cache, &cv);
+  if (rc != ELITEKV_OK) return rc;
+  return ekv_launch_append_slots(L, cache, cv, k_e, c, slot, pos, T, (cudaStream_t)stream);
+}
+
 extern "C" int elitekv_project_append(const elitekv_layer* L, const elitekv_cache* cache, const void* x,
                                       const int32_t* seq_id, const int32_t* pos, int64_t T,
                                       elitekv_stream_t stream) {

@@ -22,10 +22,10 @@
 
 namespace {
 
-template <bool kVec>
+template <bool kVec, bool kSlots>
 __global__ void __launch_bounds__(256)
 append_kernel(const AppendArgs a) {
-  append_tokens<kVec>(a, blockIdx.x, gridDim.x);
+  append_tokens<kVec, kSlots>(a, blockIdx.x, gridDim.x);
 }
 
 // ------------------------------------------------------------------ staged form (prefill)
@@ -54,6 +54,7 @@ __device__ __forceinline__ void bulk_store_row(void* dst, uint32_t src, uint32_t
 // block's it-th group, and the whole block rotates and stores the group loaded kLag
 // iterations earlier.  A stage is loaded again kStages - kLag iterations after its stores were issued;
 // the issuing lane first waits until those stores have read the stage.
+template <bool kSlots>
 __global__ void __launch_bounds__(kStagedThreads)
 append_staged_kernel(const AppendArgs a, int G) {
   extern __shared__ __align__(128) unsigned char smem_stage[];
@@ -85,15 +86,9 @@ append_staged_kernel(const AppendArgs a, int G) {
       long long row = -1;
       int p = 0;
       if (t < a.T) {                    // every lane owns a token here, so every lane records its own fault
-        const int sq = a.seq_id[t];
-        p = a.pos[t];
-        if (p < 0 || p >= a.max_pos) {
-          ekv_record(a.status, ELITEKV_ERR_BAD_POSITION, sq, p);
-        } else {
-          int code, detail;
-          row = ekv_token_row(a.cv, sq, p, &code, &detail);
-          if (row < 0) ekv_record(a.status, code, sq, detail);
-        }
+        int code, d0 = 0, d1 = 0;
+        row = append_find<kSlots>(a, t, &p, &code, &d0, &d1);
+        if (code != 0) ekv_record(a.status, code, d0, d1);
       }
       s_row[st][lane] = row;
       s_pos[st][lane] = p;
@@ -172,11 +167,11 @@ append_staged_kernel(const AppendArgs a, int G) {
 
 }  // namespace
 
-int ekv_launch_append(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv,
-                      const void* k_e, const void* c, const int32_t* seq_id, const int32_t* pos,
-                      long long T, cudaStream_t st) {
-  if (T == 0) return ELITEKV_OK;
-  const AppendArgs a = append_args(L, cache, cv, k_e, c, seq_id, pos, T);
+namespace {
+
+template <bool kSlots>
+int launch_append(const elitekv_layer* L, const AppendArgs& a, cudaStream_t st) {
+  const long long T = a.T;
   // prefill-sized calls: the staged form (rows are whole 16-byte units, and the buffers are
   // 16-byte aligned: checked at the entry point)
   const long long tok_bytes = (long long)L->n_h * L->r * 4 + (long long)L->d_c * 2;
@@ -186,17 +181,31 @@ int ekv_launch_append(const elitekv_layer* L, const elitekv_cache* cache, const 
     const size_t smem = (size_t)kStages * G * tok_bytes;
     const long long n_groups = (T + G - 1) / G;
     const long long want = (long long)L->sm_count * kBlocksPerSm;
-    EKV_CUDA_OK(ekv_allow_smem(append_staged_kernel, smem));
-    append_staged_kernel<<<(unsigned)(n_groups < want ? n_groups : want), kStagedThreads, smem, st>>>(a, G);
+    EKV_CUDA_OK(ekv_allow_smem(append_staged_kernel<kSlots>, smem));
+    append_staged_kernel<kSlots><<<(unsigned)(n_groups < want ? n_groups : want), kStagedThreads, smem, st>>>(a, G);
     EKV_CUDA_OK(cudaGetLastError());
     return ELITEKV_OK;
   }
   const long long groups = (T + kTok - 1) / kTok;
   long long blocks = groups < (long long)L->sm_count * 8 ? groups : (long long)L->sm_count * 8;
   if (append_vec_ok(L))
-    append_kernel<true><<<(unsigned)blocks, 256, 0, st>>>(a);
+    append_kernel<true, kSlots><<<(unsigned)blocks, 256, 0, st>>>(a);
   else
-    append_kernel<false><<<(unsigned)blocks, 256, 0, st>>>(a);
+    append_kernel<false, kSlots><<<(unsigned)blocks, 256, 0, st>>>(a);
   EKV_CUDA_OK(cudaGetLastError());
   return ELITEKV_OK;
+}
+
+}  // namespace
+
+int ekv_launch_append(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv,
+                      const void* k_e, const void* c, const int32_t* seq_id, const int32_t* pos,
+                      long long T, cudaStream_t st) {
+  if (T == 0) return ELITEKV_OK;
+  return launch_append<false>(L, append_args(L, cache, cv, k_e, c, seq_id, pos, T), st);
+}
+
+int ekv_launch_append_slots(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const void* k_e,
+                            const void* c, const int64_t* slot, const int32_t* pos, long long T, cudaStream_t st) {
+  return launch_append<true>(L, append_args(L, cache, cv, k_e, c, (const int32_t*)slot, pos, T), st);
 }

@@ -19,17 +19,46 @@ struct AppendArgs {
   int32_t* status;
 };
 
-// cache row of token t, or -1 (fault recorded by thread 0)
-__device__ __forceinline__ long long append_row(const AppendArgs& a, long long t, int* p_out) {
-  const int s = a.seq_id[t], p = a.pos[t];
-  *p_out = p;
-  if (p < 0 || p >= a.max_pos) {
-    if (threadIdx.x == 0) ekv_record(a.status, ELITEKV_ERR_BAD_POSITION, s, p);
+// Cache row of token t, or -1 with what there is to record (code 0: nothing).  kSlots: `seq_id` is the slot map
+// (int64 rows), a negative slot is padding.
+template <bool kSlots>
+__device__ __forceinline__ long long append_find(const AppendArgs& a, long long t, int* p_out, int* code, int* d0, int* d1) {
+  *code = 0;
+  if (kSlots) {
+    const long long row = ((const long long*)a.seq_id)[t];
+    if (row < 0) return -1;
+    const int p = a.pos[t];
+    *p_out = p;
+    const long long rows = a.cv.page_table ? a.cv.num_pages << a.cv.page_shift : (long long)a.cv.n_seqs * a.cv.max_ctx;
+    if (p >= 0 && p < a.max_pos && row < rows) return row;
+    *code = ELITEKV_ERR_BAD_POSITION;
+    *d0 = (int)t;
+    *d1 = p;
     return -1;
   }
-  int code, detail;
-  const long long row = ekv_token_row(a.cv, s, p, &code, &detail);
-  if (row < 0 && threadIdx.x == 0) ekv_record(a.status, code, s, detail);
+  const int s = a.seq_id[t], p = a.pos[t];
+  *p_out = p;
+  *d0 = s;
+  if (p < 0 || p >= a.max_pos) {
+    *code = ELITEKV_ERR_BAD_POSITION;
+    *d1 = p;
+    return -1;
+  }
+  int c, detail;
+  const long long row = ekv_token_row(a.cv, s, p, &c, &detail);
+  if (row < 0) {
+    *code = c;
+    *d1 = detail;
+  }
+  return row;
+}
+
+// cache row of token t, or -1 (fault recorded by thread 0)
+template <bool kSlots>
+__device__ __forceinline__ long long append_row(const AppendArgs& a, long long t, int* p_out) {
+  int code, d0 = 0, d1 = 0;
+  const long long row = append_find<kSlots>(a, t, p_out, &code, &d0, &d1);
+  if (code != 0 && threadIdx.x == 0) ekv_record(a.status, code, d0, d1);
   return row;
 }
 
@@ -46,7 +75,7 @@ constexpr int kTok = 2;      // tokens a block works on at once (independent 16-
                              // extra loads in flight bring)
 
 // Tokens blk, blk + n_blk, ... of the call, kTok at a time.
-template <bool kVec>
+template <bool kVec, bool kSlots = false>
 __device__ __forceinline__ void append_tokens(const AppendArgs& a, unsigned blk, unsigned n_blk) {
   const int n_pairs = a.n_h * a.r;
   const int n_vec = a.d_c >> 3;
@@ -59,7 +88,7 @@ __device__ __forceinline__ void append_tokens(const AppendArgs& a, unsigned blk,
     for (int e = 0; e < kTok; ++e) {
       tk[e] = t0 + (long long)e * n_blk;
       p[e] = 0;
-      row[e] = tk[e] < a.T ? append_row(a, tk[e], &p[e]) : -1;
+      row[e] = tk[e] < a.T ? append_row<kSlots>(a, tk[e], &p[e]) : -1;
     }
     for (int v = threadIdx.x; v < n_items; v += blockDim.x) {
       // loads of all tokens first, then the arithmetic and the stores

@@ -139,6 +139,12 @@ inline cudaError_t ekv_launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block,
   return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
 }
 
+// Whether the current device is the layer's: its tables and status word live there
+inline bool ekv_on_device(const elitekv_layer* L) {
+  int device = -1;
+  return cudaGetDevice(&device) == cudaSuccess && device == L->device;
+}
+
 // Where a (sequence, position) lives in the cache planes.
 struct CacheView {
   const int32_t* page_table;
@@ -175,6 +181,8 @@ int ekv_make_view(const elitekv_cache* cache, CacheView* out);
 int ekv_launch_append(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv,
                       const void* k_e, const void* c, const int32_t* seq_id, const int32_t* pos,
                       long long T, cudaStream_t st);
+int ekv_launch_append_slots(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const void* k_e,
+                            const void* c, const int64_t* slot, const int32_t* pos, long long T, cudaStream_t st);
 int ekv_launch_project_append(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv,
                               const void* x, const int32_t* seq_id, const int32_t* pos, long long T,
                               cudaStream_t st);

@@ -203,6 +203,7 @@ extern "C" const char* elitekv_strerror(int status) {
     case ELITEKV_ERR_BAD_POSITION: return "position or sequence outside the cache";
     case ELITEKV_ERR_STATIC_SCRATCH_EXCEEDED:
       return "scratch need exceeds the built-in array of elitekv_decode_static";
+    case ELITEKV_ERR_NO_PAGES: return "fewer free pages than the step needs";
     default: return "unknown status";
   }
 }

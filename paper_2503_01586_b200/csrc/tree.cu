@@ -1,0 +1,209 @@
+// Attention of a tree of drafted tokens over the cache: entry points and the kernel for any shape.
+//
+//   s[i,h,t] = scale (q_rope[i,h] . k_rope[t,h] + q_abs[i,h] . c[t]),   p = softmax over the tokens that node i sees,
+//   acc[i,h] = sum_t p c[t]   (W_uv follows in the combine, csrc/combine.cu)
+//
+// Node i sees every committed token (t < n - nodes) and the nodes j of its mask (t = n - nodes + j).
+//
+// tree_generic_kernel: a warp per (sequence, node, head) and split of the tokens.  Lanes hold the latent axis, eight
+// coordinates at a time; queries and the running sum (fp32) lie in shared memory.  Tokens that the row does not see
+// are skipped, so that nothing of theirs is read.  Bound: the warp-wide sum of every token (latency), a row's own
+// read of the whole cache (L2).  It serves what the tensor-core form does not cover.
+#include "tree.cuh"
+
+namespace {
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct GenArgs {
+  const bf16 *q_rope, *q_abs, *rope, *latent;
+  const int32_t *seq_lens, *n_nodes;
+  const uint64_t* mask;
+  CacheView cv;
+  int B, m, n_h, r2, d_c, kw, voff, vw, splits;
+  long long max_len;
+  float scale_log2e;
+  float *part_acc, *part_ml;
+  int32_t *seq_first, *counters, *status;
+  int n_counters;
+};
+
+// the items of the combine and its counters; lengths that do not fit are recorded once
+__global__ void tree_generic_prep_kernel(const GenArgs a) {
+  ekv_pdl_wait();
+  ekv_pdl_trigger();
+  const long long t = (long long)blockIdx.x * blockDim.x + threadIdx.x, step = (long long)gridDim.x * blockDim.x;
+  for (long long b = t; b <= a.B; b += step) {
+    a.seq_first[b] = (int)b * a.splits;
+    if (b < a.B && tree_lens(a.seq_lens, a.n_nodes, (int)b, a.m, a.max_len).bad)
+      ekv_record(a.status, ELITEKV_ERR_BAD_POSITION, (int)b, a.seq_lens[b]);
+  }
+  for (long long k = t; k < a.n_counters; k += step) a.counters[k] = 0;
+}
+
+__global__ void tree_generic_kernel(const GenArgs a) {
+  extern __shared__ float s_row[];
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float* const s_q = s_row + (size_t)warp * (a.kw + a.vw);      // scaled by nothing: bf16 values as floats
+  float* const s_acc = s_q + a.kw;
+  const long long rows = (long long)a.B * a.m * a.n_h, row = (long long)blockIdx.x * warps + warp;
+  const int split = blockIdx.y;
+  ekv_pdl_wait();
+  ekv_pdl_trigger();
+  if (row >= rows) return;
+  const int h = (int)(row % a.n_h), i = (int)(row / a.n_h % a.m), b = (int)(row / a.n_h / a.m);
+  const TreeLens len = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
+  const int per = (len.n + a.splits - 1) / a.splits;
+  const int t0 = min(split * per, len.n), t1 = i < len.nodes ? min(t0 + per, len.n) : t0;
+  const int prefix = len.n - len.nodes;
+  const unsigned long long mask = i < len.nodes ? a.mask[(long long)b * a.m + i] : 0ull;
+  for (int k = lane; k < a.kw; k += 32) s_q[k] = __bfloat162float(a.q_abs[row * a.kw + k]);
+  for (int k = lane; k < a.vw; k += 32) s_acc[k] = 0.f;
+  __syncwarp();
+  float m_run = -1e30f, l_run = 0.f;
+  for (int t = t0; t < t1; ++t) {
+    if (t >= prefix && !(mask >> (t - prefix) & 1)) continue;
+    int code, detail;
+    long long at = ekv_token_row(a.cv, b, t, &code, &detail);
+    if (at < 0) {
+      if (lane == 0) ekv_record(a.status, code, b, detail);
+      at = 0;                                  // page 0, as in the other attention kernels
+    }
+    const bf16* c = a.latent + at * a.d_c;
+    float s = 0.f;
+    for (int k = lane * 8; k < a.kw; k += 256) {
+      const uint4 x = __ldg((const uint4*)(c + k));
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __bfloat1622float2(*(const bf162*)&w[e]);
+        s = fmaf(f.x, s_q[k + 2 * e], s);
+        s = fmaf(f.y, s_q[k + 2 * e + 1], s);
+      }
+    }
+    for (int k = lane; k < a.r2; k += 32)
+      s = fmaf(__bfloat162float(a.q_rope[row * a.r2 + k]), __bfloat162float(a.rope[(at * a.n_h + h) * a.r2 + k]), s);
+    s = warp_sum(s) * a.scale_log2e;
+    const float m_new = fmaxf(m_run, s), corr = exp2f(m_run - m_new), p = exp2f(s - m_new);
+    l_run = fmaf(l_run, corr, p);
+    m_run = m_new;
+    for (int k = lane * 8; k < a.vw; k += 256) {
+      const uint4 x = __ldg((const uint4*)(c + a.voff + k));
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __bfloat1622float2(*(const bf162*)&w[e]);
+        s_acc[k + 2 * e] = fmaf(p, f.x, s_acc[k + 2 * e] * corr);
+        s_acc[k + 2 * e + 1] = fmaf(p, f.y, s_acc[k + 2 * e + 1] * corr);
+      }
+    }
+  }
+  __syncwarp();
+  const long long item = (long long)b * a.splits + split, at = (item * a.m + i) * a.n_h + h;
+  for (int k = lane; k < a.vw; k += 32) a.part_acc[at * a.vw + k] = s_acc[k];
+  if (lane == 0) {
+    a.part_ml[at * 2] = m_run;
+    a.part_ml[at * 2 + 1] = l_run;
+  }
+}
+
+// Splits: enough warps for the device, at most 16 partial results a row
+int generic_splits(const elitekv_layer* L, int B, int m) {
+  const long long rows = (long long)B * m * L->n_h, want = 16ll * L->sm_count;
+  const long long s = (want + rows - 1) / rows;
+  return (int)(s > 16 ? 16 : s);
+}
+
+struct GenCarve {
+  size_t first, ml, acc, slice, cnt, total;
+};
+GenCarve generic_carve(const elitekv_layer* L, int B, int m) {
+  const size_t items = (size_t)B * generic_splits(L, B, m), rows = (size_t)m * L->n_h;
+  GenCarve c;
+  size_t o = 0;
+  c.first = o; o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
+  c.ml = o;    o = align256(o + sizeof(float) * 2 * items * rows);
+  c.acc = o;   o = align256(o + sizeof(float) * items * rows * L->vw);
+  c.slice = o; o = align256(o + ekv_combine_scratch_bytes(L, B) * m);
+  c.cnt = o;   o = align256(o + sizeof(int32_t) * (size_t)ekv_combine_counters(L, B) * m);
+  c.total = o;
+  return c;
+}
+
+}  // namespace
+
+size_t ekv_tree_generic_bytes(const elitekv_layer* L, int B, int m) { return generic_carve(L, B, m).total; }
+
+int ekv_launch_tree_generic(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const TreeCall& c, cudaStream_t st) {
+  const GenCarve w = generic_carve(L, c.B, c.m);
+  unsigned char* const base = (unsigned char*)c.workspace;
+  const size_t per_warp = sizeof(float) * ((size_t)L->kw + L->vw);
+  int warps = 8;
+  while (warps > 1 && per_warp * warps > (size_t)L->smem_optin) warps >>= 1;
+  if (per_warp * warps > (size_t)L->smem_optin) return ELITEKV_ERR_UNSUPPORTED_SHAPE;
+  GenArgs a;
+  a.q_rope = (const bf16*)c.q_rope;
+  a.q_abs = (const bf16*)c.q_abs;
+  a.rope = (const bf16*)cache->rope;
+  a.latent = (const bf16*)cache->latent;
+  a.seq_lens = c.seq_lens;
+  a.n_nodes = c.n_nodes;
+  a.mask = c.mask;
+  a.cv = cv;
+  a.B = c.B;
+  a.m = c.m;
+  a.n_h = L->n_h;
+  a.r2 = 2 * L->r;
+  a.d_c = L->d_c;
+  a.kw = L->kw;
+  a.voff = L->voff;
+  a.vw = L->vw;
+  a.splits = generic_splits(L, c.B, c.m);
+  a.max_len = cv.max_ctx;
+  a.scale_log2e = L->scale * 1.4426950408889634f;
+  a.part_acc = (float*)(base + w.acc);
+  a.part_ml = (float*)(base + w.ml);
+  a.seq_first = (int32_t*)(base + w.first);
+  a.counters = (int32_t*)(base + w.cnt);
+  a.n_counters = ekv_combine_counters(L, c.B) * c.m;
+  a.status = L->d_status;
+  const int n_prep = c.B + 1 > a.n_counters ? c.B + 1 : a.n_counters;
+  const int prep_blocks = (n_prep + 255) / 256;
+  EKV_CUDA_OK(ekv_launch_pdl(tree_generic_prep_kernel, dim3(prep_blocks < 64 ? prep_blocks : 64), dim3(256), 0, st, a));
+  const long long rows = (long long)c.B * c.m * L->n_h, blocks = (rows + warps - 1) / warps;
+  if (blocks > 0x7fffffffll) return ELITEKV_ERR_UNSUPPORTED_SHAPE;
+  EKV_CUDA_OK(ekv_allow_smem(tree_generic_kernel, per_warp * warps));
+  EKV_CUDA_OK(ekv_launch_pdl(tree_generic_kernel, dim3((unsigned)blocks, (unsigned)a.splits), dim3(32 * warps), per_warp * warps, st, a));
+  DecodeScratch ws = {};
+  ws.rows = c.m;
+  ws.seq_first = a.seq_first;
+  ws.part_ml = a.part_ml;
+  ws.part_acc = a.part_acc;
+  ws.slice_out = (float*)(base + w.slice);
+  ws.counters = a.counters;
+  return ekv_launch_combine(L, c.B, ws, c.out, st);
+}
+
+extern "C" int elitekv_attend_tree_workspace_size(const elitekv_layer* L, int32_t B, int32_t m, size_t* bytes) {
+  if (!L || !bytes || B <= 0 || m < 1 || m > ELITEKV_MAX_TREE_NODES) return ELITEKV_ERR_INVALID_ARG;
+  *bytes = ekv_tree_generic_bytes(L, B, m);
+  return ELITEKV_OK;
+}
+
+extern "C" int elitekv_attend_tree(const elitekv_layer* L, const elitekv_cache* cache, const void* q_rope, const void* q_abs,
+                                   const int32_t* seq_lens, const int32_t* n_nodes, const uint64_t* tree_mask, int32_t B, int32_t m,
+                                   void* workspace, size_t workspace_bytes, void* out, elitekv_stream_t stream) {
+  if (!L || !cache || !q_abs || !seq_lens || !tree_mask || !workspace || !out || (L->r > 0 && !q_rope)) return ELITEKV_ERR_INVALID_ARG;
+  if (B <= 0 || B > cache->n_seqs || m < 1 || m > ELITEKV_MAX_TREE_NODES) return ELITEKV_ERR_INVALID_ARG;
+  if (((uintptr_t)q_abs & 15) || ((uintptr_t)q_rope & 15) || ((uintptr_t)out & 3) || ((uintptr_t)tree_mask & 7) || !ekv_on_device(L))
+    return ELITEKV_ERR_INVALID_ARG;
+  CacheView cv;
+  int rc = ekv_make_view(cache, &cv);
+  if (rc != ELITEKV_OK) return rc;
+  size_t need = 0;
+  rc = elitekv_attend_tree_workspace_size(L, B, m, &need);
+  if (rc != ELITEKV_OK) return rc;
+  if (((uintptr_t)workspace & 255) || workspace_bytes < need) return ELITEKV_ERR_WORKSPACE_TOO_SMALL;
+  const TreeCall c{q_rope, q_abs, seq_lens, n_nodes, tree_mask, B, m, workspace, out};
+  return ekv_launch_tree_generic(L, cache, cv, c, (cudaStream_t)stream);
+}
