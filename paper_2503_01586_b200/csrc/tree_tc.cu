@@ -1,0 +1,1067 @@
+// Attention of a tree of drafted tokens on the tensor cores (sm_100a: tcgen05, TMEM, TMA).
+//
+// All heads and nodes of a sequence read the same latent rows, so that one sequence is two dense products over its
+// cached tokens:
+//     S [rows x tokens]  = Q_abs [rows x kw] . C_k^T          (+ the per-head rope dot products)
+//     O [rows x vw]      = P [rows x tokens] . C_v            P = 2^(S - ref), bf16
+// with rows = heads x nodes, head by head (row = head * m + node: the rope rows of a warp's 32 rows are a few heads').
+// From about five nodes on (7B, 75 %) they are bound by the tensor cores and by what L2 hands to the SMs, below that by
+// the cache's bytes.  An O of 128 rows has 1536 columns, three times what TMEM holds, so the products are not fused in
+// one block: P goes through L2, 2 bytes per row and token, which costs less than exchanging partial scores between
+// blocks that split the latent axis, and both products are plain streams of operands.
+//
+// Work units, taken by persistent workers (a pair of blocks on 256 rows, or one block where 128 rows are enough) from
+// ONE ordered list, by an atomic counter:
+//     score unit  (piece, 256 tokens)           S tile over the whole kw, softmax terms, P tile to the ring in L2
+//     value unit  (piece, 256 latent columns)   O tile over the piece's tokens, to the partial result
+// A piece is (row block, up to kPiece tokens of a sequence).  The list interleaves the score units of piece j with the
+// value units of piece j - D, so that P and the piece's cache rows are read again while L2 holds them.  A unit waits only
+// for units before it in the list, and a worker that is not resident has claimed nothing: some resident worker can always
+// go on, whatever else runs on the device.
+//
+// Softmax reference.  P is bf16 and O fp32: both have 8 exponent bits, so the reference of 2^(S - ref) only has to keep
+// the exponents in range.  It is 0 while the largest score of (row, 128 tokens) is within 2^+-64, else a multiple of
+// 64 near it.  All tiles of a row agree on it unless scores are extreme; the block that finishes a piece's last
+// score unit looks, and brings P of rows that do not agree to the largest reference: a factor of a power of two, exact.
+// The sums are of the rounded P, so that their rounding cancels where one token dominates.
+//
+// Pieces of one run add into the run's partial result in order (fp32, read and written by the owner of the value unit):
+// results do not depend on scheduling, and the partial results' number does not grow with the context.  Runs are cut by the
+// prep kernel, on the device, where the lengths are.
+//
+// Tokens that a row does not see: their scores are dropped by a select, P = 0.  In the value product 0 times a value that
+// is not finite would spread it to every row, so the drafted tokens' rows (and the rest of the last 64 tokens) pass a
+// warp that clears such values before the tensor core reads them, and notes the nodes: rows that see one become NaN.
+//
+// Every wait is bounded; when one runs out the block records ELITEKV_ERR_TIMEOUT and leaves.
+#include "tc_ptx.cuh"
+#include "tree.cuh"
+
+namespace {
+
+constexpr int kRows = 128;              // rows per block
+constexpr int kTile = 256;              // tokens of a score unit, latent columns of a value unit
+constexpr int kPiece = 2048;            // most tokens of a piece
+constexpr int kHalfTiles = kPiece / 128;
+constexpr int kSlots = 64;              // pieces in the ring
+constexpr int kMostAhead = kSlots - 8;  // D at most
+constexpr int kTreeThreads = 384;       // warp 0 loads, 1 MMA, 2 clears drafted rows, 3 claims units, 4-11 epilogue
+constexpr int kEpiThreads = 256;
+constexpr int kQueue = 4;
+constexpr int kUnitWords = 16;
+constexpr int kMaxStages = 6;
+constexpr int kABytes = kRows * 128;
+
+enum { kScore = 0, kValue = 1, kStop = 2 };
+
+struct TreeUnit {
+  int type, b, rb, tok0, len, idx, slot, gen, n, nodes, run, k, pad[4];
+};
+static_assert(sizeof(TreeUnit) == kUnitWords * 4, "published word by word");
+
+struct TreeTcArgs {
+  CacheView cv;
+  const bf16 *q_rope, *rope;
+  const uint64_t* mask;
+  int m, n_h, r2, kw, vw, hb, n_rb, n_ct, box_s, box_v;
+  float scale_log2e;
+  bf16* P;                    // [slot][CG][128][kPiece]
+  float2* stats;              // [slot][CG][2 tiles][128]: (reference, sum) of a row's 128 tokens
+  float2* pref;               // [slot][CG][128]: the same of the piece
+  float2* cstate;             // [run][rb][ct][CG][2][128]: of the run so far
+  int *s_cnt, *ready, *v_done, *chain;
+  float *part_acc, *part_ml;
+  const int* hdr;             // [0] claim counter, [1] runs, [2] pieces (row blocks included), [3] D
+  const int4* runs;           // [run][2]: (b, first token, tokens, pieces), (n, nodes, ., .)
+  int32_t* status;
+};
+
+struct __align__(8) TreeBars {
+  uint64_t full[kMaxStages], empty[kMaxStages], spec[kMaxStages], fixed[kMaxStages];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t q_full[kQueue], q_empty[kQueue];
+};
+
+template <int CG>
+struct TreeSmem {
+  static constexpr int b_bytes = kTile / CG * 128;            // 256 (128) token rows, or 64 tokens of 256 (128) columns
+  static constexpr int stage = kABytes + b_bytes;
+  static constexpr int n_stages = CG == 2 ? 6 : 4;
+  static constexpr int misc = sizeof(TreeBars) + kQueue * sizeof(TreeUnit) + kQueue * 16 + 64;
+  static constexpr int total = n_stages * stage + misc + 1024;
+};
+
+__device__ __forceinline__ int ld_acquire(const int* p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_release(int* p, int v) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+// generic and asynchronous accesses of global and shared memory, both ways
+__device__ __forceinline__ void fence_proxy_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// until *p has reached target (counters wrap nowhere near: a call's counts start at zero)
+__device__ __forceinline__ bool poll_global(const int* p, int target, volatile int* abort_flag, int why) {
+  for (unsigned i = 0; i < (1u << 22); ++i) {
+    if (ld_acquire(p) >= target) return true;
+    if ((i & 63) == 63 && *abort_flag) return false;
+  }
+  if (*abort_flag == 0) *abort_flag = why;
+  return false;
+}
+__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, int why) {
+  for (unsigned i = 0; i < kWaitLimit; ++i) {
+    if (__any_sync(0xffffffffu, mbar_try_wait_cluster(bar, parity))) return true;
+    if ((i & 1023) == 1023 && __any_sync(0xffffffffu, *abort_flag != 0)) return false;
+  }
+  if (*abort_flag == 0) *abort_flag = why;
+  return false;
+}
+__device__ __forceinline__ void st_global_v8(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+// cache row of token t of sequence b; a page outside the pool counts as page 0 (recorded where `status` is given)
+__device__ __forceinline__ long long tree_row(const CacheView& cv, int b, int t, int32_t* status) {
+  if (cv.page_table == nullptr) return (long long)b * cv.max_ctx + t;
+  int page = cv.page_table[(long long)b * cv.max_pages_per_seq + (t >> cv.page_shift)];
+  if (page < 0 || page >= cv.num_pages) {
+    if (status) ekv_record(status, ELITEKV_ERR_BAD_PAGE, b, page);
+    page = 0;
+  }
+  return ((long long)page << cv.page_shift) + (t & cv.page_mask);
+}
+
+// The list of units, walked forward: block j of the list holds the score units of piece j and the value units of
+// piece j - D.  A piece walker stands on one piece (run, k-th piece of the run, row block).
+struct PieceWalk {
+  int p, run, k, rb;
+  int4 r, r2;
+};
+__device__ __forceinline__ void walk_load(PieceWalk& w, const TreeTcArgs& a, int n_runs) {
+  if (w.run < n_runs) {
+    w.r = __ldcg(a.runs + 2 * w.run);
+    w.r2 = __ldcg(a.runs + 2 * w.run + 1);
+  }
+}
+__device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int n_runs) {
+  ++w.p;
+  if (++w.rb < a.n_rb) return;
+  w.rb = 0;
+  if (++w.k < w.r.w) return;
+  w.k = 0;
+  ++w.run;
+  walk_load(w, a, n_runs);
+}
+__device__ __forceinline__ int walk_len(const PieceWalk& w) { return min(kPiece, w.r.z - w.k * kPiece); }
+
+template <int CG, int R2>
+__global__ void __launch_bounds__(kTreeThreads, 1)
+tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_p, const TreeTcArgs a) {
+  using SM = TreeSmem<CG>;
+  constexpr int NST = SM::n_stages;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  TreeBars* const bars = (TreeBars*)(base + NST * SM::stage);
+  volatile TreeUnit* const s_unit = (volatile TreeUnit*)(bars + 1);
+  // [unit][block of the pair]: nodes with values that are not finite among the columns that the block loads
+  volatile unsigned long long* const s_nf = (volatile unsigned long long*)(s_unit + kQueue);
+  uint32_t* const s_tmem = (uint32_t*)(s_nf + 2 * kQueue);
+  volatile int* const s_abort = (volatile int*)(s_tmem + 1);
+  volatile int* const s_verdict = s_abort + 1;      // [2]
+  volatile int* const s_last = s_verdict + 2;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NST; ++i) {
+      mbar_init(smem_u32(&bars->full[i]), 1);
+      mbar_init(smem_u32(&bars->empty[i]), 1);
+      mbar_init(smem_u32(&bars->spec[i]), 1);
+      mbar_init(smem_u32(&bars->fixed[i]), CG);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars->acc_full[i]), 1);
+      mbar_init(smem_u32(&bars->acc_empty[i]), 8 * CG);
+    }
+    for (int i = 0; i < kQueue; ++i) {
+      mbar_init(smem_u32(&bars->q_full[i]), kUnitWords);
+      mbar_init(smem_u32(&bars->q_empty[i]), 1 + 10 * CG);
+    }
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  }
+  if (warp == 1) {
+    if (CG == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *s_tmem;
+  ekv_pdl_wait();
+  ekv_pdl_trigger();
+
+  const int nkc = (a.kw + 63) >> 6;
+  // a published unit: what every role waits for, reads and gives back
+  unsigned q_pos = 0;
+  auto q_slot = [&]() { return q_pos % kQueue; };
+  auto q_parity = [&]() { return (q_pos / kQueue) & 1u; };
+  auto release_unit = [&]() {                        // one lane of a warp
+    const uint32_t bar = smem_u32(&bars->q_empty[q_slot()]);
+    if (CG == 2) mbar_arrive_cluster(map_to_cta(bar, 0)); else mbar_arrive(bar);
+  };
+
+  if (warp == 0) {
+    // ============================================================== loads
+    bool ok = true;
+    unsigned pos = 0;
+    for (;; ++q_pos) {
+      ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 1);
+      if (!ok) break;
+      const volatile TreeUnit* u = s_unit + q_slot();
+      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, n = u->n, gen = u->gen;
+      const int prefix = n - u->nodes;
+      __syncwarp();
+      if (lane == 0) release_unit();
+      if (type == kStop) break;
+      if (type == kScore) {
+        const int t_all = tok0 + idx * kTile, t0 = t_all + (int)rank * (kTile / CG) * (CG == 2 ? 1 : 0);
+        const int bs = a.box_s, n_box = kTile / CG / bs;
+        // boxes of this block (lane j: box j), of the whole tile for the bytes that the first block expects
+        const int mine = min(n_box, max(0, (n - t0 + bs - 1) / bs));
+        const int all = min(kTile / bs, (n - t_all + bs - 1) / bs);
+        int row = 0;
+        if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
+        const int h0 = (rb * CG + (int)rank) * a.hb;
+        const uint32_t bytes = (uint32_t)(CG * a.m * a.hb * 128 + all * bs * 128);
+        for (int kc = 0; kc < nkc && ok; ++kc, ++pos) {
+          const unsigned st = pos % NST;
+          ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 2);
+          if (!ok) break;
+          const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage);
+          const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
+          if (elect_one()) {
+            if (rank == 0) mbar_expect_tx(fb, bytes);
+            if (CG == 2) tma_load_4d_pair(dst, &map_q, kc * 64, 0, h0, b, cfb); else tma_load_4d(dst, &map_q, kc * 64, 0, h0, b, cfb);
+          }
+          __syncwarp();
+          for (int j = 0; j < mine; ++j) {
+            const int y = __shfl_sync(0xffffffffu, row, j);
+            if (elect_one()) {
+              if (CG == 2) tma_load_2d_pair(dst + kABytes + j * bs * 128, &map_k, kc * 64, y, cfb);
+              else tma_load_2d(dst + kABytes + j * bs * 128, &map_k, kc * 64, y, cfb);
+            }
+            __syncwarp();
+          }
+        }
+      } else {
+        // P of the piece is complete when each block's rows are
+        ok = __all_sync(0xffffffffu, lane != 0 || poll_global(a.ready + slot, (gen + 1) * CG, s_abort, 3));
+        if (!ok) break;
+        fence_proxy_all();
+        const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6, x0 = idx * kTile + (int)rank * 128 * (CG == 2 ? 1 : 0);
+        // 64-column chunks that exist, of this block and of all
+        const int left = a.vw - idx * kTile;
+        const int ch_all = min(kTile / 64, (left + 63) >> 6);
+        const int ch = CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;
+        int row = 0;
+        for (int ks = 0; ks < ks_n && ok; ++ks, ++pos) {
+          const int b0 = ks * per;                    // first box of the step
+          if ((b0 & 31) == 0) {
+            const int t = tok0 + (b0 + lane) * bv;
+            row = t < n && t < tok0 + len ? (int)tree_row(a.cv, b, t, nullptr) : 0;
+          }
+          const int t0 = tok0 + ks * 64, boxes = min(per, (n - t0 + bv - 1) / bv);
+          const bool special = t0 + 64 > prefix;
+          const unsigned st = pos % NST;
+          ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 4);
+          if (!ok) break;
+          const uint32_t fb = smem_u32(&bars->full[st]), sb = smem_u32(&bars->spec[st]), dst = smem_u32(base + st * SM::stage);
+          const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
+          if (elect_one()) {
+            if (rank == 0) mbar_expect_tx(fb, (uint32_t)(CG * kABytes + (special ? 0 : ch_all * boxes * bv * 128)));
+            if (special) mbar_expect_tx(sb, (uint32_t)(ch * boxes * bv * 128));
+            const int y = (slot * CG + (int)rank) * kRows;
+            if (CG == 2) tma_load_2d_pair(dst, &map_p, ks * 64, y, cfb); else tma_load_2d(dst, &map_p, ks * 64, y, cfb);
+          }
+          __syncwarp();
+          for (int j = 0; j < boxes; ++j) {
+            const int y = __shfl_sync(0xffffffffu, row, (b0 + j) & 31);
+            if (elect_one()) {
+              for (int c = 0; c < ch; ++c) {
+                const uint32_t d = dst + kABytes + c * 8192 + j * bv * 128;
+                if (special || CG == 1) tma_load_2d(d, &map_v, x0 + c * 64, y, special ? sb : fb);
+                else tma_load_2d_pair(d, &map_v, x0 + c * 64, y, cfb);
+              }
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) break;
+    }
+  } else if (warp == 1) {
+    // ============================================================== products (the first block's warp, for both)
+    if (rank == 0) {
+      constexpr uint32_t idesc_s = make_idesc(kRows * CG, kTile, 0, 0), idesc_v = make_idesc(kRows * CG, kTile, 0, 1);
+      constexpr uint32_t hi_sw = desc_hi(1024, 2);
+      const uint32_t base16 = (smem_u32(base) >> 4) & 0x3FFFu;
+      bool ok = true;
+      unsigned pos = 0, fix_bits = 0;
+      for (;; ++q_pos) {
+        ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 5);
+        if (!ok) break;
+        const volatile TreeUnit* u = s_unit + q_slot();
+        const int type = u->type, tok0 = u->tok0, len = u->len, prefix = u->n - u->nodes;
+        __syncwarp();
+        if (lane == 0) release_unit();
+        if (type == kStop) break;
+        const unsigned buf = q_pos & 1;
+        ok = warp_wait_cluster(smem_u32(&bars->acc_empty[buf]), ((q_pos >> 1) & 1) ^ 1, s_abort, 6);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + buf * kTile;
+        const int steps = type == kScore ? nkc : (len + 63) >> 6;
+        for (int ks = 0; ks < steps; ++ks, ++pos) {
+          const unsigned st = pos % NST;
+          ok = warp_wait(smem_u32(&bars->full[st]), (pos / NST) & 1, s_abort, 7);
+          if (ok && type == kValue && tok0 + ks * 64 + 64 > prefix) {
+            ok = warp_wait_cluster(smem_u32(&bars->fixed[st]), fix_bits >> st & 1, s_abort, 8);
+            fix_bits ^= 1u << st;
+          }
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t la = (base16 + st * (SM::stage >> 4)) | (1u << 16);
+          // scores: 64 latents of 256 tokens, K-major; values: 64 tokens of 256 columns, 8 KB from one 64-column chunk to the next
+          const uint32_t lb = (base16 + ((st * SM::stage + kABytes) >> 4)) | (type == kScore ? 1u << 16 : (8192u >> 4) << 16);
+          const uint32_t step_b = type == kScore ? 2 : 128;
+          const uint32_t idesc = type == kScore ? idesc_s : idesc_v;
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (CG == 2) tc_mma_pair(d, la + 2 * k, hi_sw, lb + step_b * k, hi_sw, idesc, (ks | k) != 0);
+              else tc_mma_w(d, la + 2 * k, hi_sw, lb + step_b * k, hi_sw, idesc, (ks | k) != 0);
+            }
+            if (CG == 2) tc_commit_pair(smem_u32(&bars->empty[st])); else tc_commit(smem_u32(&bars->empty[st]));
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (elect_one()) {
+          if (CG == 2) tc_commit_pair(smem_u32(&bars->acc_full[buf])); else tc_commit(smem_u32(&bars->acc_full[buf]));
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 2) {
+    // ============================================================== drafted rows of the value product
+    bool ok = true;
+    unsigned pos = 0, spec_bits = 0;
+    for (;; ++q_pos) {
+      ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 9);
+      if (!ok) break;
+      const volatile TreeUnit* u = s_unit + q_slot();
+      const int type = u->type, tok0 = u->tok0, len = u->len, idx = u->idx, n = u->n, prefix = n - u->nodes;
+      if (type == kStop) break;
+      if (type == kScore) {
+        pos += nkc;
+      } else {
+        const int ks_n = (len + 63) >> 6;
+        const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
+        const int ch = CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;
+        unsigned nf_lo = 0, nf_hi = 0;
+        for (int ks = 0; ks < ks_n; ++ks, ++pos) {
+          const int t0 = tok0 + ks * 64;
+          if (t0 + 64 <= prefix) continue;
+          const unsigned st = pos % NST;
+          ok = warp_wait(smem_u32(&bars->spec[st]), spec_bits >> st & 1, s_abort, 10);
+          spec_bits ^= 1u << st;
+          if (!ok) break;
+          const int r0 = max(prefix - t0, 0);
+          const int vecs = (64 - r0) * 8;
+          for (int c = 0; c < ch; ++c) {
+            uint4* const rows = (uint4*)(base + st * SM::stage + kABytes + c * 8192) + r0 * 8;
+            for (int e = lane; e < vecs; e += 32) {
+              const int t = t0 + r0 + (e >> 3);
+              if (t >= n) {
+                rows[e] = make_uint4(0, 0, 0, 0);
+                continue;
+              }
+              uint4 x = rows[e];
+              uint32_t w[4] = {x.x, x.y, x.z, x.w};
+              bool bad = false;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; bad = true; }
+                if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0xffffu; bad = true; }
+              }
+              if (bad) {
+                rows[e] = make_uint4(w[0], w[1], w[2], w[3]);
+                const int j = t - prefix;
+                if (j < 32) nf_lo |= 1u << j; else nf_hi |= 1u << (j - 32);
+              }
+            }
+          }
+          if (t0 + 64 >= n || ks == ks_n - 1) {       // the last of the unit: the note goes first
+            const unsigned lo = __reduce_or_sync(0xffffffffu, nf_lo), hi = __reduce_or_sync(0xffffffffu, nf_hi);
+            // to both blocks: a block's rows meet the columns of both
+            if (lane == 0) {
+              const uint32_t to = smem_u32((const void*)(s_nf + 2 * q_slot() + rank));
+              if (CG == 2) {
+#pragma unroll
+                for (int c2 = 0; c2 < 2; ++c2) {
+                  st_cluster_u32(map_to_cta(to, c2), lo);
+                  st_cluster_u32(map_to_cta(to + 4, c2), hi);
+                }
+              } else {
+                s_nf[2 * q_slot()] = (unsigned long long)hi << 32 | lo;
+              }
+            }
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (CG == 2) mbar_arrive_cluster(map_to_cta(smem_u32(&bars->fixed[st]), 0)); else mbar_arrive(smem_u32(&bars->fixed[st]));
+          }
+        }
+        if (!ok) break;
+      }
+      __syncwarp();
+      if (lane == 0) release_unit();
+    }
+  } else if (warp == 3) {
+    // ============================================================== units (the first block's warp, for both)
+    if (rank == 0) {
+      const int n_runs = __ldcg(a.hdr + 1), n_pieces = __ldcg(a.hdr + 2), ahead = __ldcg(a.hdr + 3);
+      PieceWalk ws{0, 0, 0, 0, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)}, wv = ws;
+      walk_load(ws, a, n_runs);
+      wv.r = ws.r;
+      wv.r2 = ws.r2;
+      int first = 0, j = 0;                    // first unit of block j
+      for (;; ++q_pos) {
+        if (!warp_wait_cluster(smem_u32(&bars->q_empty[q_slot()]), q_parity() ^ 1, s_abort, 11)) break;
+        int unit = 0;
+        if (lane == 0) unit = atomicAdd((int*)a.hdr, 1);
+        unit = __shfl_sync(0xffffffffu, unit, 0);
+        int n_s = 0, n_v = 0;
+        bool stop = false;
+        for (;;) {
+          n_s = j < n_pieces ? (walk_len(ws) + kTile - 1) / kTile : 0;
+          n_v = j >= ahead ? a.n_ct : 0;
+          stop = j >= n_pieces + ahead;
+          if (stop || unit < first + n_s + n_v) break;
+          first += n_s + n_v;
+          if (j < n_pieces) walk_next(ws, a, n_runs);
+          if (j >= ahead) walk_next(wv, a, n_runs);
+          ++j;
+        }
+        const int at = unit - first;
+        const bool score = at < n_s;
+        const PieceWalk& w = score ? ws : wv;
+        int word = 0;
+        switch (lane) {
+          case 0: word = stop ? kStop : score ? kScore : kValue; break;
+          case 1: word = w.r.x; break;
+          case 2: word = w.rb; break;
+          case 3: word = w.r.y + w.k * kPiece; break;
+          case 4: word = walk_len(w); break;
+          case 5: word = score ? at : at - n_s; break;
+          case 6: word = w.p % kSlots; break;
+          case 7: word = w.p / kSlots; break;
+          case 8: word = w.r2.x; break;
+          case 9: word = w.r2.y; break;
+          case 10: word = w.run; break;
+          case 11: word = w.k; break;
+        }
+        if (lane < kUnitWords) {
+          const uint32_t to = smem_u32((const void*)(s_unit + q_slot())) + 4 * lane, bar = smem_u32(&bars->q_full[q_slot()]);
+          if (CG == 2) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              st_cluster_u32(map_to_cta(to, c), (uint32_t)word);
+              mbar_arrive_cluster(map_to_cta(bar, c));
+            }
+          } else {
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(word) : "memory");
+            mbar_arrive(bar);
+          }
+        }
+        __syncwarp();
+        if (stop) break;
+      }
+    }
+  } else {
+    // ============================================================== epilogue: thread = (row, half of the columns)
+    const int quarter = warp & 3, ch = (warp - 4) >> 2, r = quarter * 32 + lane;
+    const bool leader = threadIdx.x == 128;
+    const uint32_t tm_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ch * 128);
+    const int hl = r / a.m, i = r - hl * a.m;
+    unsigned turn = 0;
+    // the leader looks, everybody gets its verdict
+    auto group = [&](auto probe) -> bool {
+      volatile int* const word = s_verdict + (turn & 1u);
+      ++turn;
+      if (leader) *word = probe() ? 1 : 0;
+      named_bar_sync(2, kEpiThreads);
+      return *word != 0;
+    };
+    auto group_bar = [&](uint32_t bar, uint32_t parity, int why) -> bool {
+      const bool ok = group([&]() {
+        for (unsigned k = 0; k < kWaitLimit; ++k) {
+          if (mbar_try_wait_cluster(bar, parity)) return true;
+          if ((k & 1023) == 1023 && *s_abort) return false;
+        }
+        if (*s_abort == 0) *s_abort = why;
+        return false;
+      });
+      if (ok) (void)mbar_try_wait_cluster(bar, parity);
+      return ok;
+    };
+    for (;; ++q_pos) {
+      if (!group_bar(smem_u32(&bars->q_full[q_slot()]), q_parity(), 12)) break;
+      const volatile TreeUnit* u = s_unit + q_slot();
+      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, gen = u->gen, n = u->n;
+      const int nodes = u->nodes, run = u->run, k_run = u->k, prefix = n - nodes;
+      if (type == kStop) break;
+      const unsigned buf = q_pos & 1;
+      const uint32_t tm = tm_row + buf * kTile, acc_bar = smem_u32(&bars->acc_full[buf]), acc_par = (q_pos >> 1) & 1;
+      const int h = (rb * CG + (int)rank) * a.hb + hl;
+      const bool real = hl < a.hb && h < a.n_h, active = real && i < nodes;
+      const unsigned long long mask = active ? a.mask[(long long)b * a.m + i] : 0ull;
+      const long long half = (long long)slot * CG + rank;        // this block's share of the slot
+      auto acc_done = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&bars->acc_empty[buf]);
+          if (CG == 2) mbar_arrive_cluster(map_to_cta(bar, 0)); else mbar_arrive(bar);
+        }
+      };
+      if (type == kScore) {
+        const int t0 = tok0 + idx * kTile + ch * 128;              // this thread's 128 tokens
+        const int nv = max(0, min(128, n - t0));
+        const int bs = a.box_s < 128 ? a.box_s : 128;
+        // rope rows: lane j knows where the tokens [j bs, (j + 1) bs) start
+        long long row_j = 0;
+        if (lane * bs < nv) row_j = tree_row(a.cv, b, t0 + lane * bs, nullptr);
+        float q[R2 > 0 ? R2 : 1];
+        const int hq = real ? h : 0, iq = real ? i : 0;
+        const bf16* const qr = a.q_rope + (((long long)b * a.m + iq) * a.n_h + hq) * a.r2;
+        if (R2 > 0) {
+#pragma unroll
+          for (int k = 0; k < R2; k += 8) {
+            const uint4 x = __ldg((const uint4*)(qr + k));
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              q[k + 2 * e] = __uint_as_float(w[e] << 16);
+              q[k + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+            }
+          }
+        }
+        // the slot's last piece is read to the end
+        if (gen > 0 && !group([&]() { return poll_global(a.v_done + slot, gen * a.n_ct * CG, s_abort, 13); })) break;
+        if (!group_bar(acc_bar, acc_par, 14)) break;
+        tc_fence_after();
+        float top = -INFINITY;
+        for (int cc = 0; cc < 4; ++cc) {
+          float v[32];
+          tc_ld32(tm + cc * 32, v);
+          tc_wait_ld();
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int tk = cc * 32 + g * 8;
+            const long long row = __shfl_sync(0xffffffffu, row_j, tk / bs) + tk % bs;
+            if (tk >= nv) continue;
+            const bf16* const kr = a.rope + (row * a.n_h + hq) * a.r2;
+            const long long pitch = (long long)a.n_h * a.r2;
+            if (R2 > 0) {
+              uint4 x[8][R2 > 0 ? R2 / 8 : 1];
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int k = 0; k < R2 / 8; ++k) x[e][k] = __ldg((const uint4*)(kr + (tk + e < nv ? e : 0) * pitch) + k);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                float s = v[g * 8 + e];
+#pragma unroll
+                for (int k = 0; k < R2 / 8; ++k) {
+                  const uint32_t w[4] = {x[e][k].x, x[e][k].y, x[e][k].z, x[e][k].w};
+#pragma unroll
+                  for (int z = 0; z < 4; ++z) {
+                    s = fmaf(__uint_as_float(w[z] << 16), q[8 * k + 2 * z], s);
+                    s = fmaf(__uint_as_float(w[z] & 0xffff0000u), q[8 * k + 2 * z + 1], s);
+                  }
+                }
+                v[g * 8 + e] = s;
+              }
+            } else {
+              for (int k = 0; k < a.r2; ++k) {
+                const float qk = __bfloat162float(qr[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[g * 8 + e] = fmaf(__bfloat162float(kr[(tk + e < nv ? e : 0) * pitch + k]), qk, v[g * 8 + e]);
+              }
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const int t = t0 + cc * 32 + e;
+            const bool seen = active && (t < prefix || (t < n && (mask >> (t - prefix) & 1)));
+            v[e] = seen ? v[e] * a.scale_log2e : -INFINITY;
+            top = fmaxf(top, v[e]);
+          }
+          tc_st32(tm + cc * 32, v);
+        }
+        tc_wait_st();
+        const float ref = top == -INFINITY || fabsf(top) <= 64.f ? 0.f : 64.f * rintf(top * (1.f / 64.f));
+        float sum = 0.f;
+        bf16* const prow = a.P + (half * kRows + r) * kPiece + idx * kTile + ch * 128;
+#pragma unroll 1
+        for (int cc = 0; cc < 4; ++cc) {
+          float v[32];
+          tc_ld32(tm + cc * 32, v);
+          tc_wait_ld();
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bf162 p = __floats2bfloat162_rn(ex2(v[2 * e] - ref), ex2(v[2 * e + 1] - ref));
+            w[e] = *(const uint32_t*)&p;
+            sum += __uint_as_float(w[e] << 16);
+            sum += __uint_as_float(w[e] & 0xffff0000u);
+          }
+          if (real) {
+            st_global_v8(prow + cc * 32, w);
+            st_global_v8(prow + cc * 32 + 16, w + 8);
+          }
+          __syncwarp();
+        }
+        acc_done();
+        a.stats[(half * kHalfTiles + idx * 2 + ch) * kRows + r] = make_float2(ref, sum);
+        fence_proxy_all();
+        __threadfence();
+        named_bar_sync(2, kEpiThreads);
+        if (leader) {
+          const int tiles = (len + kTile - 1) / kTile;
+          const int before = atomicAdd(a.s_cnt + half, 1);
+          __threadfence();
+          *s_last = before == tiles - 1;
+        }
+        named_bar_sync(2, kEpiThreads);
+        if (*s_last) {
+          // the piece's rows agree on a reference
+          const int tiles = 2 * ((len + kTile - 1) / kTile);
+          if (ch == 0) {
+            const float2* const st = a.stats + half * kHalfTiles * kRows + r;
+            float2 x[kHalfTiles];
+#pragma unroll
+            for (int t = 0; t < kHalfTiles; ++t) x[t] = t < tiles ? __ldcg(st + t * kRows) : make_float2(0.f, 0.f);
+            float m_ref = -1e30f;
+#pragma unroll
+            for (int t = 0; t < kHalfTiles; ++t)
+              if (x[t].y != 0.f) m_ref = fmaxf(m_ref, x[t].x);
+            float total = 0.f;
+#pragma unroll
+            for (int t = 0; t < kHalfTiles; ++t) {
+              if (x[t].y == 0.f) continue;
+              const float f = x[t].x == m_ref ? 1.f : exp2f(x[t].x - m_ref);
+              total = fmaf(x[t].y, f, total);
+              if (f != 1.f && real) {
+                uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * 128);
+                for (int e = 0; e < 64; ++e) {
+                  const uint32_t w = __ldcg(pr + e);
+                  const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
+                  pr[e] = *(const uint32_t*)&y;
+                }
+              }
+            }
+            a.pref[half * kRows + r] = make_float2(m_ref, total);
+          }
+          fence_proxy_all();
+          __threadfence();
+          named_bar_sync(2, kEpiThreads);
+          if (leader) {
+            a.s_cnt[half] = 0;
+            add_release(a.ready + slot, 1);
+          }
+        }
+      } else {
+        const long long ci = ((long long)run * a.n_rb + rb) * a.n_ct + idx;
+        // the piece before in the run is in the partial result
+        if (k_run > 0 && !group([&]() { return poll_global(a.chain + ci, k_run * CG, s_abort, 15); })) break;
+        if (!group_bar(acc_bar, acc_par, 16)) break;
+        tc_fence_after();
+        const float2 mine = __ldcg(a.pref + half * kRows + r);
+        float2* const state = a.cstate + ((ci * CG + rank) * 2 + ch) * kRows + r;
+        float2 now = mine;
+        float f_old = 0.f, f_new = 1.f;
+        if (k_run > 0) {
+          const float2 old = __ldcg(state);
+          now.x = fmaxf(old.x, mine.x);
+          f_old = exp2f(old.x - now.x);
+          f_new = exp2f(mine.x - now.x);
+          now.y = old.y * f_old + mine.y * f_new;
+        }
+        // (values before the drafted ones are what all rows see; a row that sees nothing adds nothing)
+        const bool special = tok0 + ((len + 63) & ~63) > prefix;
+        const bool spoiled = special && ((s_nf[2 * q_slot()] | (CG == 2 ? s_nf[2 * q_slot() + 1] : 0ull)) & mask) != 0;
+        const bool none = mine.y == 0.f;
+        *state = now;
+        const long long prow = ((long long)run * a.m + i) * a.n_h + h;
+        if (real && idx == 0 && ch == 0) {
+          a.part_ml[prow * 2] = now.x;
+          a.part_ml[prow * 2 + 1] = now.y;
+        }
+        const int c0 = idx * kTile + ch * 128;
+        float* const out = a.part_acc + prow * a.vw + c0;
+#pragma unroll 1
+        for (int cc = 0; cc < 4; ++cc) {
+          float v[32];
+          tc_ld32(tm + cc * 32, v);
+          const int cols = a.vw - c0 - cc * 32;          // columns left, a multiple of 8
+          float4 o[8];
+          if (k_run > 0 && real) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = e * 4 < cols ? __ldcg((const float4*)(out + cc * 32) + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          tc_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = spoiled ? __uint_as_float(0x7fffffffu) : none ? 0.f : v[e];
+          if (k_run > 0 && real) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              v[4 * e] = v[4 * e] * f_new + o[e].x * f_old;
+              v[4 * e + 1] = v[4 * e + 1] * f_new + o[e].y * f_old;
+              v[4 * e + 2] = v[4 * e + 2] * f_new + o[e].z * f_old;
+              v[4 * e + 3] = v[4 * e + 3] * f_new + o[e].w * f_old;
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (real && e * 8 < cols) st_global_v8(out + cc * 32 + e * 8, (const uint32_t*)v + e * 8);
+          __syncwarp();
+        }
+        acc_done();
+        __threadfence();
+        named_bar_sync(2, kEpiThreads);
+        if (leader) {
+          add_release(a.chain + ci, 1);
+          add_release(a.v_done + slot, 1);
+        }
+      }
+      if (lane == 0) release_unit();
+    }
+  }
+
+  // ============================================================== teardown
+  tc_fence_before();
+  __syncthreads();
+  if (*s_abort) drain_after_abort();
+  if (threadIdx.x == 0 && *s_abort) ekv_record(a.status, ELITEKV_ERR_TIMEOUT, (int)blockIdx.x | (*s_abort << 16), 0);
+  __syncwarp();
+  if (CG == 2) cluster_sync_all();         // the tensor core and the peer's roles are through with this block's memory
+  if (warp == 1) {
+    tc_fence_after();
+    if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ runs
+struct TreePrepArgs {
+  const int32_t *seq_lens, *n_nodes;
+  int B, m, n_rb, n_ct, want, workers;
+  long long max_len;
+  int* hdr;
+  int4* runs;
+  int32_t* seq_first;
+  int* zero;
+  int n_zero;
+  int32_t* counters;
+  int n_counters;
+  int32_t* status;
+};
+
+// One block cuts every sequence into runs of equal length (a multiple of 256 tokens): about `want` of them beside one
+// per sequence, so that the value units fill the workers a few times over.  The rest of the grid zeroes the counters.
+__global__ void __launch_bounds__(256)
+tree_prep_kernel(const TreePrepArgs a) {
+  ekv_pdl_wait();
+  ekv_pdl_trigger();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (blockIdx.x > 0) {
+    const int t = (blockIdx.x - 1) * 256 + tid, step = (gridDim.x - 1) * 256;
+    for (int k = t; k < a.n_zero; k += step) a.zero[k] = 0;
+    for (int k = t; k < a.n_counters; k += step) a.counters[k] = 0;
+    return;
+  }
+  __shared__ long long s_sum[8];
+  __shared__ int s_cnt[3][8];
+  long long total = 0;
+  for (int b = tid; b < a.B; b += 256) {
+    const TreeLens t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
+    if (t.bad) ekv_record(a.status, ELITEKV_ERR_BAD_POSITION, b, a.seq_lens[b]);
+    if (t.nodes > 0) total += t.n;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  if (lane == 0) s_sum[warp] = total;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < 8; ++w) total += s_sum[w];
+  const long long per = (total + a.want - 1) / a.want;
+  const long long up = (per + 255) / 256 * 256;
+  const int run_len = (int)(up < 256 ? 256 : up > (1ll << 30) ? 1ll << 30 : up);      // (no sequence is longer than 2^30)
+  int run0 = 0, item0 = 0, score0 = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 256) {
+    const int b = b0 + tid;
+    TreeLens t{0, 0, false};
+    int runs = 0, len = 256, items = 0, scores = 0;
+    if (b < a.B) t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
+    if (t.nodes > 0) {                        // a sequence without nodes has only padding: zero rows
+      runs = (t.n + run_len - 1) / run_len;
+      len = ((t.n + runs - 1) / runs + 255) / 256 * 256;
+      runs = (t.n + len - 1) / len;
+      const int last = t.n - (runs - 1) * len;
+      items = (runs - 1) * ((len + kPiece - 1) / kPiece) + (last + kPiece - 1) / kPiece;
+      scores = (t.n + 255) / 256;
+    }
+    int v[3] = {runs, items, scores}, x[3];
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+      x[e] = v[e];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x[e], o);
+        if (lane >= o) x[e] += y;
+      }
+      if (lane == 31) s_cnt[e][warp] = x[e];
+    }
+    __syncthreads();
+    int at = run0 + x[0] - v[0];
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) at += s_cnt[0][w];
+      run0 += s_cnt[0][w];
+      item0 += s_cnt[1][w];
+      score0 += s_cnt[2][w];
+    }
+    if (b < a.B) {
+      a.seq_first[b] = at;
+      for (int k = 0; k < runs; ++k) {
+        const int tok = k * len, l = min(len, t.n - tok);
+        a.runs[2 * (at + k)] = make_int4(b, tok, l, (l + kPiece - 1) / kPiece);
+        a.runs[2 * (at + k) + 1] = make_int4(t.n, t.nodes, 0, 0);
+      }
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {
+    a.seq_first[a.B] = run0;
+    const long long pieces = (long long)item0 * a.n_rb, units = (long long)score0 * a.n_rb + pieces * a.n_ct;
+    // how far the score units go ahead of the value units: what the workers hold two and a half times over
+    long long d = units > 0 ? (5ll * a.workers * pieces + 2 * units - 1) / (2 * units) : 1;
+    d = d < 1 ? 1 : d > kMostAhead ? kMostAhead : d;
+    a.hdr[0] = 0;
+    a.hdr[1] = run0;
+    a.hdr[2] = (int)pieces;
+    a.hdr[3] = (int)d;
+  }
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// rows of a block are whole heads; one block where it holds all of them, else pairs
+struct TreeShape {
+  int cg, hb, n_rb, n_ct, workers, want;
+};
+TreeShape tree_shape(const elitekv_layer* L, int m) {
+  TreeShape s;
+  const int most = kRows / m, blocks = (L->n_h + most - 1) / most;
+  s.cg = blocks == 1 ? 1 : 2;
+  s.n_rb = (blocks + s.cg - 1) / s.cg;
+  s.hb = (L->n_h + s.n_rb * s.cg - 1) / (s.n_rb * s.cg);
+  s.n_ct = (L->vw + kTile - 1) / kTile;
+  s.workers = L->sm_count / s.cg;
+  s.want = 4 * s.workers / (s.n_rb * s.n_ct);
+  if (s.want < 1) s.want = 1;
+  return s;
+}
+
+struct TreeCarve {
+  size_t hdr, runs, first, zero, n_zero, stats, pref, cstate, P, ml, acc, slice, cnt, total;
+  size_t max_runs;
+};
+TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
+  TreeCarve c;
+  const size_t rows = (size_t)m * L->n_h;
+  c.max_runs = (size_t)B + s.want;
+  const size_t chains = c.max_runs * s.n_rb * s.n_ct;
+  size_t o = 0;
+  c.hdr = o;    o = align256(o + 16);
+  c.runs = o;   o = align256(o + c.max_runs * 32);
+  c.first = o;  o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
+  c.n_zero = (size_t)kSlots * (s.cg + 2) + chains;
+  c.zero = o;   o = align256(o + sizeof(int) * c.n_zero);
+  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * kHalfTiles * kRows);
+  c.pref = o;   o = align256(o + sizeof(float2) * kSlots * s.cg * kRows);
+  c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * 2 * kRows);
+  c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
+  c.ml = o;     o = align256(o + sizeof(float) * 2 * c.max_runs * rows);
+  c.acc = o;    o = align256(o + sizeof(float) * c.max_runs * rows * L->vw);
+  c.slice = o;  o = align256(o + ekv_combine_scratch_bytes(L, B) * m);
+  c.cnt = o;    o = align256(o + sizeof(int32_t) * (size_t)ekv_combine_counters(L, B) * m);
+  c.total = o;
+  return c;
+}
+
+// bf16 [rows][cols] with `pitch` elements from row to row, box [box_rows][64], 128-byte swizzle
+int make_map_pitch(CUtensorMap* m, const void* ptr, unsigned long long rows, unsigned long long cols, unsigned long long pitch, unsigned box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return ELITEKV_ERR_CUDA;
+  cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch * sizeof(bf16)};
+  cuuint32_t box[2] = {64, box_rows}, estr[2] = {1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
+}
+// queries [B][m][n_h][kw] seen as (sequence, head, node, latent): a box is `hb` heads of m nodes each
+int make_map_queries(CUtensorMap* map, const void* ptr, int B, int m, int n_h, int kw, int hb) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return ELITEKV_ERR_CUDA;
+  cuuint64_t dims[4] = {(cuuint64_t)kw, (cuuint64_t)m, (cuuint64_t)n_h, (cuuint64_t)B};
+  cuuint64_t strides[3] = {(cuuint64_t)n_h * kw * 2, (cuuint64_t)kw * 2, (cuuint64_t)m * n_h * kw * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)m, (cuuint32_t)hb, 1}, estr[4] = {1, 1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
+}
+
+unsigned long long plane_rows(const CacheView& cv) {
+  return cv.page_table ? (unsigned long long)cv.num_pages << cv.page_shift : (unsigned long long)cv.max_ctx * cv.n_seqs;
+}
+
+}  // namespace
+
+size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m) { return tree_carve(L, tree_shape(L, m), B, m).total; }
+
+// Pages of 8 tokens and more: a box of the copy engine is whole 1024-byte groups of the swizzle.  Box coordinates have 32 bits.
+int ekv_tree_tc_supported(const elitekv_layer* L, const CacheView* cv) {
+  if (TreeSmem<1>::total > L->smem_optin || TreeSmem<2>::total > L->smem_optin) return 0;
+  if (cv && cv->page_table && (1 << cv->page_shift) < 8) return 0;
+  if (cv && (plane_rows(*cv) >= (1ull << 31) || cv->max_ctx > (1ll << 30))) return 0;
+  return 1;
+}
+
+int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const TreeCall& c, cudaStream_t st) {
+  const TreeShape s = tree_shape(L, c.m);
+  const TreeCarve w = tree_carve(L, s, c.B, c.m);
+  unsigned char* const base = (unsigned char*)c.workspace;
+  const int page = cv.page_table ? 1 << cv.page_shift : 1 << 30;
+  TreeTcArgs a;
+  a.cv = cv;
+  a.q_rope = (const bf16*)c.q_rope;
+  a.rope = (const bf16*)cache->rope;
+  a.mask = c.mask;
+  a.m = c.m;
+  a.n_h = L->n_h;
+  a.r2 = 2 * L->r;
+  a.kw = L->kw;
+  a.vw = L->vw;
+  a.hb = s.hb;
+  a.n_rb = s.n_rb;
+  a.n_ct = s.n_ct;
+  a.box_s = page < 128 ? page : 128;
+  a.box_v = page < 64 ? page : 64;
+  a.scale_log2e = L->scale * 1.4426950408889634f;
+  a.P = (bf16*)(base + w.P);
+  a.stats = (float2*)(base + w.stats);
+  a.pref = (float2*)(base + w.pref);
+  a.cstate = (float2*)(base + w.cstate);
+  a.s_cnt = (int*)(base + w.zero);
+  a.ready = a.s_cnt + kSlots * s.cg;
+  a.v_done = a.ready + kSlots;
+  a.chain = a.v_done + kSlots;
+  a.part_acc = (float*)(base + w.acc);
+  a.part_ml = (float*)(base + w.ml);
+  a.hdr = (const int*)(base + w.hdr);
+  a.runs = (const int4*)(base + w.runs);
+  a.status = L->d_status;
+  CUtensorMap m_q, m_k, m_v, m_p;
+  const unsigned long long rows = plane_rows(cv);
+  int rc = make_map_queries(&m_q, c.q_abs, c.B, c.m, L->n_h, L->kw, s.hb);
+  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_k, cache->latent, rows, L->kw, L->d_c, a.box_s);
+  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
+  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, kRows);
+  if (rc != ELITEKV_OK) return rc;
+  TreePrepArgs p;
+  p.seq_lens = c.seq_lens;
+  p.n_nodes = c.n_nodes;
+  p.B = c.B;
+  p.m = c.m;
+  p.n_rb = s.n_rb;
+  p.n_ct = s.n_ct;
+  p.want = s.want;
+  p.workers = s.workers;
+  p.max_len = cv.max_ctx;
+  p.hdr = (int*)(base + w.hdr);
+  p.runs = (int4*)(base + w.runs);
+  p.seq_first = (int32_t*)(base + w.first);
+  p.zero = a.s_cnt;
+  p.n_zero = (int)w.n_zero;
+  p.counters = (int32_t*)(base + w.cnt);
+  p.n_counters = ekv_combine_counters(L, c.B) * c.m;
+  p.status = L->d_status;
+  const int n_max = p.n_zero > p.n_counters ? p.n_zero : p.n_counters, zero_blocks = (n_max + 1023) / 1024;
+  EKV_CUDA_OK(ekv_launch_pdl(tree_prep_kernel, dim3(1 + (zero_blocks < 32 ? zero_blocks : 32)), dim3(256), 0, st, p));
+  const int smem = s.cg == 2 ? TreeSmem<2>::total : TreeSmem<1>::total;
+  auto launch = [&](auto kern) -> int {
+    EKV_CUDA_OK(ekv_allow_smem(kern, smem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(s.workers * s.cg));
+    cfg.blockDim = dim3(kTreeThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)s.cg;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    EKV_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, m_q, m_k, m_v, m_p, a));
+    return ELITEKV_OK;
+  };
+  if (s.cg == 2)
+    rc = a.r2 == 8 ? launch(tree_tc_kernel<2, 8>) : a.r2 == 16 ? launch(tree_tc_kernel<2, 16>)
+         : a.r2 == 32 ? launch(tree_tc_kernel<2, 32>) : launch(tree_tc_kernel<2, 0>);
+  else
+    rc = a.r2 == 8 ? launch(tree_tc_kernel<1, 8>) : a.r2 == 16 ? launch(tree_tc_kernel<1, 16>)
+         : a.r2 == 32 ? launch(tree_tc_kernel<1, 32>) : launch(tree_tc_kernel<1, 0>);
+  if (rc != ELITEKV_OK) return rc;
+  EKV_CUDA_OK(cudaGetLastError());
+  DecodeScratch ws = {};
+  ws.rows = c.m;
+  ws.seq_first = p.seq_first;
+  ws.part_ml = a.part_ml;
+  ws.part_acc = a.part_acc;
+  ws.slice_out = (float*)(base + w.slice);
+  ws.counters = p.counters;
+  return ekv_launch_combine(L, c.B, ws, c.out, st);
+}
