@@ -2,9 +2,11 @@
 //
 // All heads and nodes of a sequence read the same latent rows, so that one sequence is two dense products over its
 // cached tokens:
-//     S [rows x tokens]  = Q_abs [rows x kw] . C_k^T          (+ the per-head rope dot products)
+//     S [rows x tokens]  = [Q_abs | Q_rope] [rows x (kw + rope)] . [C_k | K_rope]^T
 //     O [rows x vw]      = P [rows x tokens] . C_v            P = 2^(S - ref), bf16
-// with rows = heads x nodes, head by head (row = head * m + node: the rope rows of a warp's 32 rows are a few heads').
+// with rows = heads x nodes, head by head.  The rope columns of a block's heads join the score product with zeros where
+// row and column belong to different heads (the prep kernel lays the queries out so): 16 nodes of a 7B layer add 4 steps
+// of 64 to 24 that way; on FP32 lanes in the epilogue they took 30 us a tile.
 // From about five nodes on (7B, 75 %) they are bound by the tensor cores and by what L2 hands to the SMs, below that by
 // the cache's bytes.  An O of 128 rows has 1536 columns, three times what TMEM holds, so the products are not fused in
 // one block: P goes through L2, 2 bytes per row and token, which costs less than exchanging partial scores between
@@ -61,9 +63,8 @@ static_assert(sizeof(TreeUnit) == kUnitWords * 4, "published word by word");
 
 struct TreeTcArgs {
   CacheView cv;
-  const bf16 *q_rope, *rope;
   const uint64_t* mask;
-  int m, n_h, r2, kw, vw, hb, n_rb, n_ct, box_s, box_v;
+  int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v;
   float scale_log2e;
   bf16* P;                    // [slot][CG][128][kPiece]
   float2* stats;              // [slot][CG][2 tiles][128]: (reference, sum) of a row's 128 tokens
@@ -139,6 +140,9 @@ __device__ __forceinline__ long long tree_row(const CacheView& cv, int b, int t,
   return ((long long)page << cv.page_shift) + (t & cv.page_mask);
 }
 
+// first rope column that a row block's score product takes: of its first head, on a 16-byte boundary
+__host__ __device__ __forceinline__ int tree_rope_col(int h0, int r2) { return h0 * r2 & ~7; }
+
 // The list of units, walked forward: block j of the list holds the score units of piece j and the value units of
 // piece j - D.  A piece walker stands on one piece (run, k-th piece of the run, row block).
 struct PieceWalk {
@@ -162,10 +166,11 @@ __device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int
 }
 __device__ __forceinline__ int walk_len(const PieceWalk& w) { return min(kPiece, w.r.z - w.k * kPiece); }
 
-template <int CG, int R2>
+template <int CG>
 __global__ void __launch_bounds__(kTreeThreads, 1)
 tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_p, const TreeTcArgs a) {
+               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_p,
+               const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r, const TreeTcArgs a) {
   using SM = TreeSmem<CG>;
   constexpr int NST = SM::n_stages;
   extern __shared__ unsigned char smem_raw[];
@@ -217,7 +222,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   ekv_pdl_wait();
   ekv_pdl_trigger();
 
-  const int nkc = (a.kw + 63) >> 6;
+  const int nkl = (a.kw + 63) >> 6, nkc = nkl + a.n_rc;       // steps of a score unit: latents, then rope columns
   // a published unit: what every role waits for, reads and gives back
   unsigned q_pos = 0;
   auto q_slot = [&]() { return q_pos % kQueue; };
@@ -249,23 +254,32 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         int row = 0;
         if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
         const int h0 = (rb * CG + (int)rank) * a.hb;
-        const uint32_t bytes = (uint32_t)(CG * a.m * a.hb * 128 + all * bs * 128);
+        const uint32_t bytes_l = (uint32_t)(CG * a.m * a.hb * 128 + all * bs * 128), bytes_r = (uint32_t)(CG * kABytes + all * bs * 128);
+        const int yq = ((b * a.n_rb + rb) * CG + (int)rank) * a.n_rc * kRows, xr = tree_rope_col(rb * CG * a.hb, a.r2);
         for (int kc = 0; kc < nkc && ok; ++kc, ++pos) {
           const unsigned st = pos % NST;
           ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 2);
           if (!ok) break;
           const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage);
           const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
+          const bool lat = kc < nkl;
+          const int xa = kc * 64, c = kc - nkl;
           if (elect_one()) {
-            if (rank == 0) mbar_expect_tx(fb, bytes);
-            if (CG == 2) tma_load_4d_pair(dst, &map_q, kc * 64, 0, h0, b, cfb); else tma_load_4d(dst, &map_q, kc * 64, 0, h0, b, cfb);
+            if (rank == 0) mbar_expect_tx(fb, lat ? bytes_l : bytes_r);
+            if (lat) {
+              if (CG == 2) tma_load_4d_pair(dst, &map_q, xa, 0, h0, b, cfb); else tma_load_4d(dst, &map_q, xa, 0, h0, b, cfb);
+            } else {
+              if (CG == 2) tma_load_2d_pair(dst, &map_qr, 0, yq + c * kRows, cfb); else tma_load_2d(dst, &map_qr, 0, yq + c * kRows, cfb);
+            }
           }
           __syncwarp();
+          const CUtensorMap* const map_b = lat ? &map_k : &map_r;
+          const int xb = lat ? xa : xr + c * 64;
           for (int j = 0; j < mine; ++j) {
             const int y = __shfl_sync(0xffffffffu, row, j);
             if (elect_one()) {
-              if (CG == 2) tma_load_2d_pair(dst + kABytes + j * bs * 128, &map_k, kc * 64, y, cfb);
-              else tma_load_2d(dst + kABytes + j * bs * 128, &map_k, kc * 64, y, cfb);
+              if (CG == 2) tma_load_2d_pair(dst + kABytes + j * bs * 128, map_b, xb, y, cfb);
+              else tma_load_2d(dst + kABytes + j * bs * 128, map_b, xb, y, cfb);
             }
             __syncwarp();
           }
@@ -555,95 +569,58 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       };
       if (type == kScore) {
         const int t0 = tok0 + idx * kTile + ch * 128;              // this thread's 128 tokens
-        const int nv = max(0, min(128, n - t0));
-        const int bs = a.box_s < 128 ? a.box_s : 128;
-        // rope rows: lane j knows where the tokens [j bs, (j + 1) bs) start
-        long long row_j = 0;
-        if (lane * bs < nv) row_j = tree_row(a.cv, b, t0 + lane * bs, nullptr);
-        float q[R2 > 0 ? R2 : 1];
-        const int hq = real ? h : 0, iq = real ? i : 0;
-        const bf16* const qr = a.q_rope + (((long long)b * a.m + iq) * a.n_h + hq) * a.r2;
-        if (R2 > 0) {
-#pragma unroll
-          for (int k = 0; k < R2; k += 8) {
-            const uint4 x = __ldg((const uint4*)(qr + k));
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              q[k + 2 * e] = __uint_as_float(w[e] << 16);
-              q[k + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-            }
-          }
-        }
         // the slot's last piece is read to the end
         if (gen > 0 && !group([&]() { return poll_global(a.v_done + slot, gen * a.n_ct * CG, s_abort, 13); })) break;
         if (!group_bar(acc_bar, acc_par, 14)) break;
         tc_fence_after();
+        // which of 32 tokens the row sees; tiles of committed tokens alone skip it
+        const bool all = t0 + 128 <= prefix;
+        auto seen_bits = [&](int t) -> unsigned {                  // tokens t .. t + 31
+          if (t + 32 <= prefix) return 0xffffffffu;
+          const int d = prefix - t;                                // committed ones in front: d of them
+          const unsigned long long v = d >= 0 ? (mask << d) | ((1ull << d) - 1ull) : d > -64 ? mask >> -d : 0ull;
+          const int left = n - t;
+          return left <= 0 ? 0u : (unsigned)v & (left >= 32 ? 0xffffffffu : (1u << left) - 1u);
+        };
         float top = -INFINITY;
+#pragma unroll 1
         for (int cc = 0; cc < 4; ++cc) {
           float v[32];
           tc_ld32(tm + cc * 32, v);
+          const unsigned bits = all ? 0xffffffffu : seen_bits(t0 + cc * 32);
           tc_wait_ld();
+          if (!all) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int tk = cc * 32 + g * 8;
-            const long long row = __shfl_sync(0xffffffffu, row_j, tk / bs) + tk % bs;
-            if (tk >= nv) continue;
-            const bf16* const kr = a.rope + (row * a.n_h + hq) * a.r2;
-            const long long pitch = (long long)a.n_h * a.r2;
-            if (R2 > 0) {
-              uint4 x[8][R2 > 0 ? R2 / 8 : 1];
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int k = 0; k < R2 / 8; ++k) x[e][k] = __ldg((const uint4*)(kr + (tk + e < nv ? e : 0) * pitch) + k);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                float s = v[g * 8 + e];
-#pragma unroll
-                for (int k = 0; k < R2 / 8; ++k) {
-                  const uint32_t w[4] = {x[e][k].x, x[e][k].y, x[e][k].z, x[e][k].w};
-#pragma unroll
-                  for (int z = 0; z < 4; ++z) {
-                    s = fmaf(__uint_as_float(w[z] << 16), q[8 * k + 2 * z], s);
-                    s = fmaf(__uint_as_float(w[z] & 0xffff0000u), q[8 * k + 2 * z + 1], s);
-                  }
-                }
-                v[g * 8 + e] = s;
-              }
-            } else {
-              for (int k = 0; k < a.r2; ++k) {
-                const float qk = __bfloat162float(qr[k]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[g * 8 + e] = fmaf(__bfloat162float(kr[(tk + e < nv ? e : 0) * pitch + k]), qk, v[g * 8 + e]);
-              }
-            }
+            for (int e = 0; e < 32; ++e) v[e] = bits >> e & 1 ? v[e] : -INFINITY;
           }
+          float t4[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const int t = t0 + cc * 32 + e;
-            const bool seen = active && (t < prefix || (t < n && (mask >> (t - prefix) & 1)));
-            v[e] = seen ? v[e] * a.scale_log2e : -INFINITY;
-            top = fmaxf(top, v[e]);
-          }
-          tc_st32(tm + cc * 32, v);
+          for (int e = 4; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], v[e]);
+          top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
         }
-        tc_wait_st();
+        top *= a.scale_log2e;
         const float ref = top == -INFINITY || fabsf(top) <= 64.f ? 0.f : 64.f * rintf(top * (1.f / 64.f));
-        float sum = 0.f;
+        float sum4[4] = {0.f, 0.f, 0.f, 0.f};
         bf16* const prow = a.P + (half * kRows + r) * kPiece + idx * kTile + ch * 128;
 #pragma unroll 1
         for (int cc = 0; cc < 4; ++cc) {
           float v[32];
           tc_ld32(tm + cc * 32, v);
+          const unsigned bits = all ? 0xffffffffu : seen_bits(t0 + cc * 32);
           tc_wait_ld();
           uint32_t w[16];
 #pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = ex2(fmaf(v[e], a.scale_log2e, -ref));
+          if (!all) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = bits >> e & 1 ? v[e] : 0.f;
+          }
+#pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const bf162 p = __floats2bfloat162_rn(ex2(v[2 * e] - ref), ex2(v[2 * e + 1] - ref));
+            const bf162 p = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
             w[e] = *(const uint32_t*)&p;
-            sum += __uint_as_float(w[e] << 16);
-            sum += __uint_as_float(w[e] & 0xffff0000u);
+            sum4[2 * (e & 1)] += __uint_as_float(w[e] << 16);
+            sum4[2 * (e & 1) + 1] += __uint_as_float(w[e] & 0xffff0000u);
           }
           if (real) {
             st_global_v8(prow + cc * 32, w);
@@ -651,6 +628,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           }
           __syncwarp();
         }
+        // (rows of padding nodes weigh nothing, whatever their queries hold)
+        const float sum = active ? (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]) : 0.f;
         acc_done();
         a.stats[(half * kHalfTiles + idx * 2 + ch) * kRows + r] = make_float2(ref, sum);
         fence_proxy_all();
@@ -785,7 +764,9 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 // ------------------------------------------------------------------ runs
 struct TreePrepArgs {
   const int32_t *seq_lens, *n_nodes;
-  int B, m, n_rb, n_ct, want, workers;
+  const bf16* q_rope;
+  bf16* qr;                   // [B][row block][block][n_rc][128][64]
+  int B, m, n_rb, n_ct, want, workers, cg, n_h, r2, hb, n_rc, zero_blocks;
   long long max_len;
   int* hdr;
   int4* runs;
@@ -798,14 +779,34 @@ struct TreePrepArgs {
 };
 
 // One block cuts every sequence into runs of equal length (a multiple of 256 tokens): about `want` of them beside one
-// per sequence, so that the value units fill the workers a few times over.  The rest of the grid zeroes the counters.
+// per sequence, so that the value units fill the workers a few times over.  Others zero the counters; the rest of the
+// grid spreads the queries' rope parts over the columns of their row block's heads.
 __global__ void __launch_bounds__(256)
 tree_prep_kernel(const TreePrepArgs a) {
   ekv_pdl_wait();
   ekv_pdl_trigger();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (blockIdx.x > a.zero_blocks) {
+    // 16 bytes of the spread queries per thread: chunk c's columns [64 c + 8 v, + 8) of a row
+    const long long vecs = (long long)a.B * a.n_rb * a.cg * a.n_rc * kRows * 8;
+    const long long step = (long long)(gridDim.x - 1 - a.zero_blocks) * 256;
+    for (long long x = (long long)(blockIdx.x - 1 - a.zero_blocks) * 256 + tid; x < vecs; x += step) {
+      const int v = (int)(x & 7), row = (int)(x >> 3) % kRows;
+      const long long y = (x >> 3) / kRows;
+      const int c = (int)(y % a.n_rc), block = (int)(y / a.n_rc % (a.n_rb * a.cg)), b = (int)(y / a.n_rc / (a.n_rb * a.cg));
+      const int hl = row / a.m, i = row - hl * a.m, h = block * a.hb + hl;
+      const int col = tree_rope_col(block / a.cg * a.cg * a.hb, a.r2) + c * 64 + v * 8 - h * a.r2;     // of the head's own 2r
+      const bool real = hl < a.hb && h < a.n_h;
+      const bf16* const q = a.q_rope + (((long long)b * a.m + i) * a.n_h + (real ? h : 0)) * a.r2;
+      __align__(16) unsigned short w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = real && col + e >= 0 && col + e < a.r2 ? ((const unsigned short*)q)[col + e] : (unsigned short)0;
+      *(uint4*)(a.qr + x * 8) = *(const uint4*)w;
+    }
+    return;
+  }
   if (blockIdx.x > 0) {
-    const int t = (blockIdx.x - 1) * 256 + tid, step = (gridDim.x - 1) * 256;
+    const int t = (blockIdx.x - 1) * 256 + tid, step = a.zero_blocks * 256;
     for (int k = t; k < a.n_zero; k += step) a.zero[k] = 0;
     for (int k = t; k < a.n_counters; k += step) a.counters[k] = 0;
     return;
@@ -887,7 +888,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // rows of a block are whole heads; one block where it holds all of them, else pairs
 struct TreeShape {
-  int cg, hb, n_rb, n_ct, workers, want;
+  int cg, hb, n_rb, n_ct, n_rc, workers, want;
 };
 TreeShape tree_shape(const elitekv_layer* L, int m) {
   TreeShape s;
@@ -896,6 +897,12 @@ TreeShape tree_shape(const elitekv_layer* L, int m) {
   s.n_rb = (blocks + s.cg - 1) / s.cg;
   s.hb = (L->n_h + s.n_rb * s.cg - 1) / (s.n_rb * s.cg);
   s.n_ct = (L->vw + kTile - 1) / kTile;
+  s.n_rc = 0;                              // 64-column steps that hold the rope columns of any row block
+  for (int rb = 0; rb < s.n_rb && L->r > 0; ++rb) {
+    const int h0 = rb * s.cg * s.hb, h1 = h0 + s.cg * s.hb < L->n_h ? h0 + s.cg * s.hb : L->n_h;
+    const int steps = h1 > h0 ? (h1 * 2 * L->r - tree_rope_col(h0, 2 * L->r) + 63) / 64 : 0;
+    s.n_rc = steps > s.n_rc ? steps : s.n_rc;
+  }
   s.workers = L->sm_count / s.cg;
   s.want = 4 * s.workers / (s.n_rb * s.n_ct);
   if (s.want < 1) s.want = 1;
@@ -903,7 +910,7 @@ TreeShape tree_shape(const elitekv_layer* L, int m) {
 }
 
 struct TreeCarve {
-  size_t hdr, runs, first, zero, n_zero, stats, pref, cstate, P, ml, acc, slice, cnt, total;
+  size_t hdr, runs, first, zero, n_zero, stats, pref, cstate, P, qr, ml, acc, slice, cnt, total;
   size_t max_runs;
 };
 TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
@@ -921,6 +928,7 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.pref = o;   o = align256(o + sizeof(float2) * kSlots * s.cg * kRows);
   c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * 2 * kRows);
   c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
+  c.qr = o;     o = align256(o + sizeof(bf16) * (size_t)B * s.n_rb * s.cg * s.n_rc * kRows * 64);
   c.ml = o;     o = align256(o + sizeof(float) * 2 * c.max_runs * rows);
   c.acc = o;    o = align256(o + sizeof(float) * c.max_runs * rows * L->vw);
   c.slice = o;  o = align256(o + ekv_combine_scratch_bytes(L, B) * m);
@@ -959,8 +967,10 @@ unsigned long long plane_rows(const CacheView& cv) {
 
 size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m) { return tree_carve(L, tree_shape(L, m), B, m).total; }
 
-// Pages of 8 tokens and more: a box of the copy engine is whole 1024-byte groups of the swizzle.  Box coordinates have 32 bits.
+// Pages of 8 tokens and more: a box of the copy engine is whole 1024-byte groups of the swizzle.  Box coordinates have 32 bits,
+// rope rows whole 16 bytes.
 int ekv_tree_tc_supported(const elitekv_layer* L, const CacheView* cv) {
+  if ((L->n_h * L->r) % 4 != 0) return 0;
   if (TreeSmem<1>::total > L->smem_optin || TreeSmem<2>::total > L->smem_optin) return 0;
   if (cv && cv->page_table && (1 << cv->page_shift) < 8) return 0;
   if (cv && (plane_rows(*cv) >= (1ull << 31) || cv->max_ctx > (1ll << 30))) return 0;
@@ -974,8 +984,6 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   const int page = cv.page_table ? 1 << cv.page_shift : 1 << 30;
   TreeTcArgs a;
   a.cv = cv;
-  a.q_rope = (const bf16*)c.q_rope;
-  a.rope = (const bf16*)cache->rope;
   a.mask = c.mask;
   a.m = c.m;
   a.n_h = L->n_h;
@@ -985,6 +993,7 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.hb = s.hb;
   a.n_rb = s.n_rb;
   a.n_ct = s.n_ct;
+  a.n_rc = s.n_rc;
   a.box_s = page < 128 ? page : 128;
   a.box_v = page < 64 ? page : 64;
   a.scale_log2e = L->scale * 1.4426950408889634f;
@@ -1001,14 +1010,27 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.hdr = (const int*)(base + w.hdr);
   a.runs = (const int4*)(base + w.runs);
   a.status = L->d_status;
-  CUtensorMap m_q, m_k, m_v, m_p;
+  CUtensorMap m_q, m_k, m_v, m_p, m_qr, m_r;
   const unsigned long long rows = plane_rows(cv);
   int rc = make_map_queries(&m_q, c.q_abs, c.B, c.m, L->n_h, L->kw, s.hb);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_k, cache->latent, rows, L->kw, L->d_c, a.box_s);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, kRows);
+  // (a layer without rope has neither; the maps are not used)
+  m_qr = m_r = m_p;
+  if (rc == ELITEKV_OK && s.n_rc > 0) {
+    rc = make_map_pitch(&m_qr, base + w.qr, (unsigned long long)c.B * s.n_rb * s.cg * s.n_rc * kRows, 64, 64, kRows);
+    if (rc == ELITEKV_OK) rc = make_map_pitch(&m_r, cache->rope, rows, (unsigned long long)L->n_h * a.r2, (unsigned long long)L->n_h * a.r2, a.box_s);
+  }
   if (rc != ELITEKV_OK) return rc;
   TreePrepArgs p;
+  p.q_rope = (const bf16*)c.q_rope;
+  p.qr = (bf16*)(base + w.qr);
+  p.cg = s.cg;
+  p.n_h = L->n_h;
+  p.r2 = a.r2;
+  p.hb = s.hb;
+  p.n_rc = s.n_rc;
   p.seq_lens = c.seq_lens;
   p.n_nodes = c.n_nodes;
   p.B = c.B;
@@ -1027,7 +1049,9 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   p.n_counters = ekv_combine_counters(L, c.B) * c.m;
   p.status = L->d_status;
   const int n_max = p.n_zero > p.n_counters ? p.n_zero : p.n_counters, zero_blocks = (n_max + 1023) / 1024;
-  EKV_CUDA_OK(ekv_launch_pdl(tree_prep_kernel, dim3(1 + (zero_blocks < 32 ? zero_blocks : 32)), dim3(256), 0, st, p));
+  p.zero_blocks = zero_blocks < 32 ? zero_blocks : 32;
+  const long long qr_blocks = ((long long)c.B * s.n_rb * s.cg * s.n_rc * kRows * 8 + 1023) / 1024;
+  EKV_CUDA_OK(ekv_launch_pdl(tree_prep_kernel, dim3((unsigned)(1 + p.zero_blocks + (qr_blocks < 1024 ? qr_blocks : 1024))), dim3(256), 0, st, p));
   const int smem = s.cg == 2 ? TreeSmem<2>::total : TreeSmem<1>::total;
   auto launch = [&](auto kern) -> int {
     EKV_CUDA_OK(ekv_allow_smem(kern, smem));
@@ -1045,15 +1069,10 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    EKV_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, m_q, m_k, m_v, m_p, a));
+    EKV_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, m_q, m_k, m_v, m_p, m_qr, m_r, a));
     return ELITEKV_OK;
   };
-  if (s.cg == 2)
-    rc = a.r2 == 8 ? launch(tree_tc_kernel<2, 8>) : a.r2 == 16 ? launch(tree_tc_kernel<2, 16>)
-         : a.r2 == 32 ? launch(tree_tc_kernel<2, 32>) : launch(tree_tc_kernel<2, 0>);
-  else
-    rc = a.r2 == 8 ? launch(tree_tc_kernel<1, 8>) : a.r2 == 16 ? launch(tree_tc_kernel<1, 16>)
-         : a.r2 == 32 ? launch(tree_tc_kernel<1, 32>) : launch(tree_tc_kernel<1, 0>);
+  rc = s.cg == 2 ? launch(tree_tc_kernel<2>) : launch(tree_tc_kernel<1>);
   if (rc != ELITEKV_OK) return rc;
   EKV_CUDA_OK(cudaGetLastError());
   DecodeScratch ws = {};
