@@ -187,7 +187,7 @@ int ekv_launch_tree_generic(const elitekv_layer* L, const elitekv_cache* cache, 
 extern "C" int elitekv_attend_tree_workspace_size(const elitekv_layer* L, int32_t B, int32_t m, size_t* bytes) {
   if (!L || !bytes || B <= 0 || m < 1 || m > ELITEKV_MAX_TREE_NODES) return ELITEKV_ERR_INVALID_ARG;
   // the cache's layout is not known here: enough for either kernel
-  const size_t g = ekv_tree_generic_bytes(L, B, m), t = ekv_tree_tc_supported(L, nullptr) ? ekv_tree_tc_bytes(L, B, m) : 0;
+  const size_t g = ekv_tree_generic_bytes(L, B, m), t = ekv_tree_tc_supported(L, B, m, nullptr) ? ekv_tree_tc_bytes(L, B, m) : 0;
   *bytes = g > t ? g : t;
   return ELITEKV_OK;
 }
@@ -207,6 +207,6 @@ extern "C" int elitekv_attend_tree(const elitekv_layer* L, const elitekv_cache* 
   if (rc != ELITEKV_OK) return rc;
   if (((uintptr_t)workspace & 255) || workspace_bytes < need) return ELITEKV_ERR_WORKSPACE_TOO_SMALL;
   const TreeCall c{q_rope, q_abs, seq_lens, n_nodes, tree_mask, B, m, workspace, out};
-  return ekv_tree_tc_supported(L, &cv) ? ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream)
+  return ekv_tree_tc_supported(L, B, m, &cv) ? ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream)
                                        : ekv_launch_tree_generic(L, cache, cv, c, (cudaStream_t)stream);
 }

@@ -33,5 +33,5 @@ size_t ekv_tree_generic_bytes(const elitekv_layer* L, int B, int m);
 int ekv_launch_tree_generic(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const TreeCall& c, cudaStream_t st);
 
 size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m);
-int ekv_tree_tc_supported(const elitekv_layer* L, const CacheView* cv);      // cv may be null: shape alone
+int ekv_tree_tc_supported(const elitekv_layer* L, int B, int m, const CacheView* cv);      // cv may be null: shape alone
 int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const TreeCall& c, cudaStream_t st);

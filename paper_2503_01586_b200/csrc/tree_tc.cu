@@ -47,12 +47,13 @@ constexpr int kPiece = 2048;            // most tokens of a piece
 constexpr int kHalfTiles = kPiece / 128;
 constexpr int kSlots = 64;              // pieces in the ring
 constexpr int kMostAhead = kSlots - 8;  // D at most
-constexpr int kTreeThreads = 384;       // warp 0 loads, 1 MMA, 2 clears drafted rows, 3 claims units, 4-11 epilogue
+constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 loads cache rows, 3 clears drafted rows, 4-11 epilogue, 12 claims units
 constexpr int kEpiThreads = 256;
-constexpr int kQueue = 4;
+constexpr int kQueue = 2;               // units claimed ahead would be late for those that wait for them
 constexpr int kUnitWords = 16;
 constexpr int kMaxStages = 6;
 constexpr int kABytes = kRows * 128;
+constexpr int kStageBytes = 4096;       // 32 rows of 128 bytes on their way out, per epilogue warp
 
 enum { kScore = 0, kValue = 1, kStop = 2 };
 
@@ -64,14 +65,15 @@ static_assert(sizeof(TreeUnit) == kUnitWords * 4, "published word by word");
 struct TreeTcArgs {
   CacheView cv;
   const uint64_t* mask;
-  int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v;
+  int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v, v3;
   float scale_log2e;
   bf16* P;                    // [slot][CG][128][kPiece]
   float2* stats;              // [slot][CG][2 tiles][128]: (reference, sum) of a row's 128 tokens
   float2* pref;               // [slot][CG][128]: the same of the piece
   float2* cstate;             // [run][rb][ct][CG][2][128]: of the run so far
   int *s_cnt, *ready, *v_done, *chain;
-  float *part_acc, *part_ml;
+  float* part_acc;            // [run][rb][CG][128][vw]
+  float2* part_ml;            // [run][rb][CG][128]
   const int* hdr;             // [0] claim counter, [1] runs, [2] pieces (row blocks included), [3] D
   const int4* runs;           // [run][2]: (b, first token, tokens, pieces), (n, nodes, ., .)
   int32_t* status;
@@ -88,8 +90,9 @@ struct TreeSmem {
   static constexpr int b_bytes = kTile / CG * 128;            // 256 (128) token rows, or 64 tokens of 256 (128) columns
   static constexpr int stage = kABytes + b_bytes;
   static constexpr int n_stages = CG == 2 ? 6 : 4;
+  static constexpr int out = 8 * kStageBytes;
   static constexpr int misc = sizeof(TreeBars) + kQueue * sizeof(TreeUnit) + kQueue * 16 + 64;
-  static constexpr int total = n_stages * stage + misc + 1024;
+  static constexpr int total = n_stages * stage + out + misc + 1024;
 };
 
 __device__ __forceinline__ int ld_acquire(const int* p) {
@@ -124,11 +127,6 @@ __device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity,
   if (*abort_flag == 0) *abort_flag = why;
   return false;
 }
-__device__ __forceinline__ void st_global_v8(void* p, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
-
 // cache row of token t of sequence b; a page outside the pool counts as page 0 (recorded where `status` is given)
 __device__ __forceinline__ long long tree_row(const CacheView& cv, int b, int t, int32_t* status) {
   if (cv.page_table == nullptr) return (long long)b * cv.max_ctx + t;
@@ -170,12 +168,13 @@ template <int CG>
 __global__ void __launch_bounds__(kTreeThreads, 1)
 tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_p,
-               const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r, const TreeTcArgs a) {
+               const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r,
+               const __grid_constant__ CUtensorMap map_ps, const __grid_constant__ CUtensorMap map_o, const TreeTcArgs a) {
   using SM = TreeSmem<CG>;
   constexpr int NST = SM::n_stages;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  TreeBars* const bars = (TreeBars*)(base + NST * SM::stage);
+  TreeBars* const bars = (TreeBars*)(base + NST * SM::stage + SM::out);
   volatile TreeUnit* const s_unit = (volatile TreeUnit*)(bars + 1);
   // [unit][block of the pair]: nodes with values that are not finite among the columns that the block loads
   volatile unsigned long long* const s_nf = (volatile unsigned long long*)(s_unit + kQueue);
@@ -199,7 +198,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
     for (int i = 0; i < kQueue; ++i) {
       mbar_init(smem_u32(&bars->q_full[i]), kUnitWords);
-      mbar_init(smem_u32(&bars->q_empty[i]), 1 + 10 * CG);
+      mbar_init(smem_u32(&bars->q_empty[i]), 1 + 11 * CG);
     }
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -233,7 +232,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   };
 
   if (warp == 0) {
-    // ============================================================== loads
+    // ============================================================== queries, P (and the bytes that a step expects)
     bool ok = true;
     unsigned pos = 0;
     for (;; ++q_pos) {
@@ -246,56 +245,95 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
-        const int t_all = tok0 + idx * kTile, t0 = t_all + (int)rank * (kTile / CG) * (CG == 2 ? 1 : 0);
-        const int bs = a.box_s, n_box = kTile / CG / bs;
-        // boxes of this block (lane j: box j), of the whole tile for the bytes that the first block expects
-        const int mine = min(n_box, max(0, (n - t0 + bs - 1) / bs));
-        const int all = min(kTile / bs, (n - t_all + bs - 1) / bs);
-        int row = 0;
-        if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
+        const int all = min(kTile / a.box_s, (n - (tok0 + idx * kTile) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
         const int h0 = (rb * CG + (int)rank) * a.hb;
-        const uint32_t bytes_l = (uint32_t)(CG * a.m * a.hb * 128 + all * bs * 128), bytes_r = (uint32_t)(CG * kABytes + all * bs * 128);
-        const int yq = ((b * a.n_rb + rb) * CG + (int)rank) * a.n_rc * kRows, xr = tree_rope_col(rb * CG * a.hb, a.r2);
-        for (int kc = 0; kc < nkc && ok; ++kc, ++pos) {
+        const uint32_t bytes_b = (uint32_t)(all * a.box_s * 128), bytes_l = (uint32_t)(CG * a.m * a.hb * 128) + bytes_b;
+        const int yq = ((b * a.n_rb + rb) * CG + (int)rank) * a.n_rc * kRows;
+        for (int kc = 0; kc < nkc; ++kc, ++pos) {
           const unsigned st = pos % NST;
           ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 2);
           if (!ok) break;
           const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage);
           const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
           const bool lat = kc < nkl;
-          const int xa = kc * 64, c = kc - nkl;
           if (elect_one()) {
-            if (rank == 0) mbar_expect_tx(fb, lat ? bytes_l : bytes_r);
+            if (rank == 0) mbar_expect_tx(fb, lat ? bytes_l : CG * kABytes + bytes_b);
             if (lat) {
-              if (CG == 2) tma_load_4d_pair(dst, &map_q, xa, 0, h0, b, cfb); else tma_load_4d(dst, &map_q, xa, 0, h0, b, cfb);
+              if (CG == 2) tma_load_4d_pair(dst, &map_q, kc * 64, 0, h0, b, cfb); else tma_load_4d(dst, &map_q, kc * 64, 0, h0, b, cfb);
             } else {
-              if (CG == 2) tma_load_2d_pair(dst, &map_qr, 0, yq + c * kRows, cfb); else tma_load_2d(dst, &map_qr, 0, yq + c * kRows, cfb);
+              const int y = yq + (kc - nkl) * kRows;
+              if (CG == 2) tma_load_2d_pair(dst, &map_qr, 0, y, cfb); else tma_load_2d(dst, &map_qr, 0, y, cfb);
             }
           }
           __syncwarp();
-          const CUtensorMap* const map_b = lat ? &map_k : &map_r;
-          const int xb = lat ? xa : xr + c * 64;
-          for (int j = 0; j < mine; ++j) {
-            const int y = __shfl_sync(0xffffffffu, row, j);
-            if (elect_one()) {
-              if (CG == 2) tma_load_2d_pair(dst + kABytes + j * bs * 128, map_b, xb, y, cfb);
-              else tma_load_2d(dst + kABytes + j * bs * 128, map_b, xb, y, cfb);
-            }
-            __syncwarp();
-          }
         }
       } else {
         // P of the piece is complete when each block's rows are
         ok = __all_sync(0xffffffffu, lane != 0 || poll_global(a.ready + slot, (gen + 1) * CG, s_abort, 3));
         if (!ok) break;
         fence_proxy_all();
-        const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6, x0 = idx * kTile + (int)rank * 128 * (CG == 2 ? 1 : 0);
-        // 64-column chunks that exist, of this block and of all
-        const int left = a.vw - idx * kTile;
-        const int ch_all = min(kTile / 64, (left + 63) >> 6);
-        const int ch = CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;
+        const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
+        const int ch_all = a.v3 ? kTile / 64 : min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);      // 64-column chunks, both blocks
+        const int y = (slot * CG + (int)rank) * kRows;
+        for (int ks = 0; ks < ks_n; ++ks, ++pos) {
+          const int t0 = tok0 + ks * 64, boxes = min(per, (n - t0 + bv - 1) / bv);
+          const bool special = t0 + 64 > prefix;
+          const unsigned st = pos % NST;
+          ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 4);
+          if (!ok) break;
+          const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage);
+          const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
+          if (elect_one()) {
+            if (rank == 0) mbar_expect_tx(fb, (uint32_t)(CG * kABytes + (special ? 0 : ch_all * boxes * bv * 128)));
+            if (CG == 2) tma_load_2d_pair(dst, &map_p, ks * 64, y, cfb); else tma_load_2d(dst, &map_p, ks * 64, y, cfb);
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok) break;
+    }
+  } else if (warp == 2) {
+    // ============================================================== cache rows
+    bool ok = true;
+    unsigned pos = 0;
+    for (;; ++q_pos) {
+      ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 17);
+      if (!ok) break;
+      const volatile TreeUnit* u = s_unit + q_slot();
+      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, n = u->n;
+      const int prefix = n - u->nodes;
+      __syncwarp();
+      if (lane == 0) release_unit();
+      if (type == kStop) break;
+      if (type == kScore) {
+        const int t0 = tok0 + idx * kTile + (CG == 2 ? (int)rank * 128 : 0);
+        const int bs = a.box_s, mine = min(kTile / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
         int row = 0;
-        for (int ks = 0; ks < ks_n && ok; ++ks, ++pos) {
+        if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
+        const int xr = tree_rope_col(rb * CG * a.hb, a.r2);
+        for (int kc = 0; kc < nkc; ++kc, ++pos) {
+          const unsigned st = pos % NST;
+          ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 18);
+          if (!ok) break;
+          const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage + kABytes);
+          const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
+          const CUtensorMap* const map_b = kc < nkl ? &map_k : &map_r;
+          const int xb = kc < nkl ? kc * 64 : xr + (kc - nkl) * 64;
+          for (int j = 0; j < mine; ++j) {
+            const int y = __shfl_sync(0xffffffffu, row, j);
+            if (elect_one()) {
+              if (CG == 2) tma_load_2d_pair(dst + j * bs * 128, map_b, xb, y, cfb);
+              else tma_load_2d(dst + j * bs * 128, map_b, xb, y, cfb);
+            }
+            __syncwarp();
+          }
+        }
+      } else {
+        const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6, x0 = idx * kTile + (CG == 2 ? (int)rank * 128 : 0);
+        const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
+        const int ch = a.v3 ? 4 / CG : CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;
+        int row = 0;
+        for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int b0 = ks * per;                    // first box of the step
           if ((b0 & 31) == 0) {
             const int t = tok0 + (b0 + lane) * bv;
@@ -304,24 +342,26 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           const int t0 = tok0 + ks * 64, boxes = min(per, (n - t0 + bv - 1) / bv);
           const bool special = t0 + 64 > prefix;
           const unsigned st = pos % NST;
-          ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 4);
+          ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 19);
           if (!ok) break;
-          const uint32_t fb = smem_u32(&bars->full[st]), sb = smem_u32(&bars->spec[st]), dst = smem_u32(base + st * SM::stage);
+          const uint32_t fb = smem_u32(&bars->full[st]), sb = smem_u32(&bars->spec[st]), dst = smem_u32(base + st * SM::stage + kABytes);
           const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
-          if (elect_one()) {
-            if (rank == 0) mbar_expect_tx(fb, (uint32_t)(CG * kABytes + (special ? 0 : ch_all * boxes * bv * 128)));
-            if (special) mbar_expect_tx(sb, (uint32_t)(ch * boxes * bv * 128));
-            const int y = (slot * CG + (int)rank) * kRows;
-            if (CG == 2) tma_load_2d_pair(dst, &map_p, ks * 64, y, cfb); else tma_load_2d(dst, &map_p, ks * 64, y, cfb);
+          if (special) {
+            if (elect_one()) mbar_expect_tx(sb, (uint32_t)(ch * boxes * bv * 128));
+            __syncwarp();
           }
-          __syncwarp();
           for (int j = 0; j < boxes; ++j) {
             const int y = __shfl_sync(0xffffffffu, row, (b0 + j) & 31);
             if (elect_one()) {
-              for (int c = 0; c < ch; ++c) {
-                const uint32_t d = dst + kABytes + c * 8192 + j * bv * 128;
-                if (special || CG == 1) tma_load_2d(d, &map_v, x0 + c * 64, y, special ? sb : fb);
-                else tma_load_2d_pair(d, &map_v, x0 + c * 64, y, cfb);
+              if (a.v3) {
+                if (special || CG == 1) tma_load_3d(dst, &map_v, 0, y, x0 >> 6, special ? sb : fb);
+                else tma_load_3d_pair(dst, &map_v, 0, y, x0 >> 6, cfb);
+              } else {
+                for (int c = 0; c < ch; ++c) {
+                  const uint32_t d = dst + c * 8192 + j * bv * 128;
+                  if (special || CG == 1) tma_load_2d(d, &map_v, x0 + c * 64, y, special ? sb : fb);
+                  else tma_load_2d_pair(d, &map_v, x0 + c * 64, y, cfb);
+                }
               }
             }
             __syncwarp();
@@ -383,7 +423,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         __syncwarp();
       }
     }
-  } else if (warp == 2) {
+  } else if (warp == 3) {
     // ============================================================== drafted rows of the value product
     bool ok = true;
     unsigned pos = 0, spec_bits = 0;
@@ -398,7 +438,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       } else {
         const int ks_n = (len + 63) >> 6;
         const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
-        const int ch = CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;
+        const int ch = CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;      // (chunks past the last column are not stored)
         unsigned nf_lo = 0, nf_hi = 0;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int t0 = tok0 + ks * 64;
@@ -459,7 +499,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       __syncwarp();
       if (lane == 0) release_unit();
     }
-  } else if (warp == 3) {
+  } else if (warp == 12) {
     // ============================================================== units (the first block's warp, for both)
     if (rank == 0) {
       const int n_runs = __ldcg(a.hdr + 1), n_pieces = __ldcg(a.hdr + 2), ahead = __ldcg(a.hdr + 3);
@@ -526,6 +566,17 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const bool leader = threadIdx.x == 128;
     const uint32_t tm_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ch * 128);
     const int hl = r / a.m, i = r - hl * a.m;
+    unsigned char* const s_out = base + NST * SM::stage + (warp - 4) * kStageBytes;      // 32 rows of 128 bytes, swizzled
+    const uint32_t out_row = smem_u32(s_out) + lane * 128;
+    // 16 bytes of this lane's row
+    auto put = [&](int j, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out_row + ((j ^ (lane & 7)) << 4)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+    };
+    // the warp's box is free again / is full
+    auto out_free = [&]() {
+      if (lane == 0) bulk_wait_group_read<0>();
+      __syncwarp();
+    };
     unsigned turn = 0;
     // the leader looks, everybody gets its verdict
     auto group = [&](auto probe) -> bool {
@@ -582,57 +633,67 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           const int left = n - t;
           return left <= 0 ? 0u : (unsigned)v & (left >= 32 ? 0xffffffffu : (1u << left) - 1u);
         };
-        float top = -INFINITY;
-#pragma unroll 1
-        for (int cc = 0; cc < 4; ++cc) {
-          float v[32];
-          tc_ld32(tm + cc * 32, v);
-          const unsigned bits = all ? 0xffffffffu : seen_bits(t0 + cc * 32);
-          tc_wait_ld();
-          if (!all) {
+        // one pass with the reference 0; another where a row's largest score is out of range
+        float ref = 0.f, sum = 0.f;
+        for (bool again = false;;) {
+          float top = -INFINITY, sum4[4] = {0.f, 0.f, 0.f, 0.f};
+          float v[2][32];
+          tc_ld32(tm, v[0]);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = bits >> e & 1 ? v[e] : -INFINITY;
+          for (int cc = 0; cc < 4; ++cc) {
+            float* const x = v[cc & 1];
+            tc_wait_ld();
+            if (cc < 3) tc_ld32(tm + (cc + 1) * 32, v[(cc + 1) & 1]);
+            if (!all) {
+              const unsigned bits = seen_bits(t0 + cc * 32);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[e] = bits >> e & 1 ? x[e] : -INFINITY;
+            }
+            if (!again) {
+              float t4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+              for (int e = 4; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], x[e]);
+              top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+            }
+            if ((cc & 1) == 0) out_free();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const bf162 p = __floats2bfloat162_rn(ex2(fmaf(x[8 * g + 2 * e], a.scale_log2e, -ref)), ex2(fmaf(x[8 * g + 2 * e + 1], a.scale_log2e, -ref)));
+                w[e] = *(const uint32_t*)&p;
+                sum4[2 * (e & 1)] += __uint_as_float(w[e] << 16);
+                sum4[2 * (e & 1) + 1] += __uint_as_float(w[e] & 0xffff0000u);
+              }
+              put((cc & 1) * 4 + g, w[0], w[1], w[2], w[3]);
+            }
+            if (cc & 1) {
+              fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_2d(&map_ps, idx * kTile + ch * 128 + (cc >> 1) * 64, (int)half * kRows + quarter * 32, smem_u32(s_out));
+                bulk_commit_group();
+              }
+            }
           }
-          float t4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-          for (int e = 4; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], v[e]);
-          top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
-        }
-        top *= a.scale_log2e;
-        const float ref = top == -INFINITY || fabsf(top) <= 64.f ? 0.f : 64.f * rintf(top * (1.f / 64.f));
-        float sum4[4] = {0.f, 0.f, 0.f, 0.f};
-        bf16* const prow = a.P + (half * kRows + r) * kPiece + idx * kTile + ch * 128;
-#pragma unroll 1
-        for (int cc = 0; cc < 4; ++cc) {
-          float v[32];
-          tc_ld32(tm + cc * 32, v);
-          const unsigned bits = all ? 0xffffffffu : seen_bits(t0 + cc * 32);
-          tc_wait_ld();
-          uint32_t w[16];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = ex2(fmaf(v[e], a.scale_log2e, -ref));
-          if (!all) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = bits >> e & 1 ? v[e] : 0.f;
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const bf162 p = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-            w[e] = *(const uint32_t*)&p;
-            sum4[2 * (e & 1)] += __uint_as_float(w[e] << 16);
-            sum4[2 * (e & 1) + 1] += __uint_as_float(w[e] & 0xffff0000u);
-          }
-          if (real) {
-            st_global_v8(prow + cc * 32, w);
-            st_global_v8(prow + cc * 32 + 16, w + 8);
-          }
+          sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+          if (again) break;
+          // (rows of padding nodes weigh nothing, whatever their queries hold)
+          top *= a.scale_log2e;
+          ref = !active || top == -INFINITY || fabsf(top) <= 64.f ? 0.f : 64.f * rintf(top * (1.f / 64.f));
+          if (__all_sync(0xffffffffu, ref == 0.f)) break;
+          again = true;
+          if (lane == 0) bulk_wait_group_all();      // both passes write the same rows
           __syncwarp();
         }
-        // (rows of padding nodes weigh nothing, whatever their queries hold)
-        const float sum = active ? (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]) : 0.f;
+        if (!active) sum = 0.f;
         acc_done();
         a.stats[(half * kHalfTiles + idx * 2 + ch) * kRows + r] = make_float2(ref, sum);
-        fence_proxy_all();
+        if (lane == 0) {
+          bulk_wait_group_all();             // the rows are in memory
+          fence_proxy_all();
+        }
         __threadfence();
         named_bar_sync(2, kEpiThreads);
         if (leader) {
@@ -647,21 +708,21 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           const int tiles = 2 * ((len + kTile - 1) / kTile);
           if (ch == 0) {
             const float2* const st = a.stats + half * kHalfTiles * kRows + r;
-            float2 x[kHalfTiles];
-#pragma unroll
-            for (int t = 0; t < kHalfTiles; ++t) x[t] = t < tiles ? __ldcg(st + t * kRows) : make_float2(0.f, 0.f);
-            float m_ref = -1e30f;
-#pragma unroll
-            for (int t = 0; t < kHalfTiles; ++t)
-              if (x[t].y != 0.f) m_ref = fmaxf(m_ref, x[t].x);
-            float total = 0.f;
-#pragma unroll
-            for (int t = 0; t < kHalfTiles; ++t) {
-              if (x[t].y == 0.f) continue;
-              const float f = x[t].x == m_ref ? 1.f : exp2f(x[t].x - m_ref);
-              total = fmaf(x[t].y, f, total);
+            float m_ref = -1e30f, total = 0.f;
+#pragma unroll 4
+            for (int t = 0; t < tiles; ++t) {
+              const float2 x = __ldcg(st + t * kRows);
+              if (x.y != 0.f) m_ref = fmaxf(m_ref, x.x);
+            }
+#pragma unroll 4
+            for (int t = 0; t < tiles; ++t) {
+              const float2 x = __ldcg(st + t * kRows);
+              if (x.y == 0.f) continue;
+              const float f = x.x == m_ref ? 1.f : exp2f(x.x - m_ref);
+              total = fmaf(x.y, f, total);
               if (f != 1.f && real) {
                 uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * 128);
+#pragma unroll 1
                 for (int e = 0; e < 64; ++e) {
                   const uint32_t w = __ldcg(pr + e);
                   const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
@@ -681,61 +742,69 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
       } else {
         const long long ci = ((long long)run * a.n_rb + rb) * a.n_ct + idx;
-        // the piece before in the run is in the partial result
-        if (k_run > 0 && !group([&]() { return poll_global(a.chain + ci, k_run * CG, s_abort, 15); })) break;
         if (!group_bar(acc_bar, acc_par, 16)) break;
         tc_fence_after();
+        // the piece before in the run is in the partial result
+        if (k_run > 0 && !group([&]() { return poll_global(a.chain + ci, k_run * CG, s_abort, 15); })) break;
         const float2 mine = __ldcg(a.pref + half * kRows + r);
         float2* const state = a.cstate + ((ci * CG + rank) * 2 + ch) * kRows + r;
+        const long long tile_row = (((long long)run * a.n_rb + rb) * CG + rank) * kRows;      // of the block's rows in the partial result
         float2 now = mine;
-        float f_old = 0.f, f_new = 1.f;
+        float f_old = 1.f, f_new = 1.f;
         if (k_run > 0) {
           const float2 old = __ldcg(state);
           now.x = fmaxf(old.x, mine.x);
           f_old = exp2f(old.x - now.x);
           f_new = exp2f(mine.x - now.x);
           now.y = old.y * f_old + mine.y * f_new;
+          if (old.y == 0.f || !real) f_old = 1.f;       // (nothing there to scale, or nobody reads it)
         }
         // (values before the drafted ones are what all rows see; a row that sees nothing adds nothing)
         const bool special = tok0 + ((len + 63) & ~63) > prefix;
         const bool spoiled = special && ((s_nf[2 * q_slot()] | (CG == 2 ? s_nf[2 * q_slot() + 1] : 0ull)) & mask) != 0;
         const bool none = mine.y == 0.f;
+        const bool scaled = __any_sync(0xffffffffu, f_old != 1.f);
         *state = now;
-        const long long prow = ((long long)run * a.m + i) * a.n_h + h;
-        if (real && idx == 0 && ch == 0) {
-          a.part_ml[prow * 2] = now.x;
-          a.part_ml[prow * 2 + 1] = now.y;
-        }
+        if (idx == 0 && ch == 0) a.part_ml[tile_row + r] = now;
         const int c0 = idx * kTile + ch * 128;
-        float* const out = a.part_acc + prow * a.vw + c0;
-#pragma unroll 1
+        float v[2][32];
+        tc_ld32(tm, v[0]);
+#pragma unroll
         for (int cc = 0; cc < 4; ++cc) {
-          float v[32];
-          tc_ld32(tm + cc * 32, v);
-          const int cols = a.vw - c0 - cc * 32;          // columns left, a multiple of 8
-          float4 o[8];
-          if (k_run > 0 && real) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = e * 4 < cols ? __ldcg((const float4*)(out + cc * 32) + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
+          float* const x = v[cc & 1];
           tc_wait_ld();
+          if (cc < 3) tc_ld32(tm + (cc + 1) * 32, v[(cc + 1) & 1]);
+          const int col = c0 + cc * 32;
+          if (col >= a.vw) continue;                      // (the same for the whole warp)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = spoiled ? __uint_as_float(0x7fffffffu) : none ? 0.f : v[e];
-          if (k_run > 0 && real) {
+          for (int e = 0; e < 32; ++e) x[e] = spoiled ? __uint_as_float(0x7fffffffu) : none ? 0.f : x[e] * f_new;
+          if (scaled) {                                   // references moved: what is there is scaled by its reader
+            const float* const o = a.part_acc + (tile_row + r) * a.vw + col;
+            for (int e = 0; e < 32; e += 4)
+              if (col + e < a.vw) {
+                const float4 y = __ldcg((const float4*)(o + e));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              v[4 * e] = v[4 * e] * f_new + o[e].x * f_old;
-              v[4 * e + 1] = v[4 * e + 1] * f_new + o[e].y * f_old;
-              v[4 * e + 2] = v[4 * e + 2] * f_new + o[e].z * f_old;
-              v[4 * e + 3] = v[4 * e + 3] * f_new + o[e].w * f_old;
-            }
+                for (int z = 0; z < 32; z += 4)
+                  if (z == e) { x[z] += y.x * f_old; x[z + 1] += y.y * f_old; x[z + 2] += y.z * f_old; x[z + 3] += y.w * f_old; }
+              }
           }
+          out_free();
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (real && e * 8 < cols) st_global_v8(out + cc * 32 + e * 8, (const uint32_t*)v + e * 8);
+          for (int g = 0; g < 8; ++g)
+            put(g, __float_as_uint(x[4 * g]), __float_as_uint(x[4 * g + 1]), __float_as_uint(x[4 * g + 2]), __float_as_uint(x[4 * g + 3]));
+          fence_proxy_async();
           __syncwarp();
+          if (lane == 0) {
+            if (k_run == 0 || scaled) tma_store_2d(&map_o, col, (int)(tile_row + quarter * 32), smem_u32(s_out));
+            else tma_add_2d(&map_o, col, (int)(tile_row + quarter * 32), smem_u32(s_out));
+            bulk_commit_group();
+          }
         }
         acc_done();
+        if (lane == 0) {
+          bulk_wait_group_all();
+          fence_proxy_all();
+        }
         __threadfence();
         named_bar_sync(2, kEpiThreads);
         if (leader) {
@@ -773,8 +842,6 @@ struct TreePrepArgs {
   int32_t* seq_first;
   int* zero;
   int n_zero;
-  int32_t* counters;
-  int n_counters;
   int32_t* status;
 };
 
@@ -808,7 +875,6 @@ tree_prep_kernel(const TreePrepArgs a) {
   if (blockIdx.x > 0) {
     const int t = (blockIdx.x - 1) * 256 + tid, step = a.zero_blocks * 256;
     for (int k = t; k < a.n_zero; k += step) a.zero[k] = 0;
-    for (int k = t; k < a.n_counters; k += step) a.counters[k] = 0;
     return;
   }
   __shared__ long long s_sum[8];
@@ -884,6 +950,255 @@ tree_prep_kernel(const TreePrepArgs a) {
   }
 }
 
+// ------------------------------------------------------------------ runs joined, W_uv
+// out[b,i,h,:] = (sum over runs 2^(m_run - M) acc_run / L) . W_uv,h: block = (head, 128 rows (b, i), a share of the latent
+// axis).  Per 64 latents the block joins the runs' fp32 rows (16 threads on 256 bytes of a row) into a bf16 head plus a
+// bf16 remainder, written as the A tile of two products with W_uv's [64 x d_h] block, which the copy engine brings three
+// steps ahead.  Blocks that share a tile's depth are a cluster; each adds its share of the columns over the others' sums in
+// block order through distributed shared memory.
+// Bound: the partial results, read once.
+constexpr int kUpThreads = 256;
+constexpr int kUpW = 4;                   // W_uv blocks in flight
+constexpr int kUpHeld = 8;                // runs whose weights a row keeps
+
+struct UpArgs {
+  const float* part_acc;
+  const float2* part_ml;
+  const int32_t* seq_first;
+  bf16* out;
+  int B, m, n_h, d_h, hb, n_half, vw;
+  int32_t* status;
+};
+struct __align__(8) UpBars {
+  uint64_t w_full[kUpW], done[2];
+};
+struct UpSmem {
+  __host__ __device__ static constexpr int a_bytes() { return 2 * 2 * kRows * 128; }                 // 2 stages of head and remainder
+  __host__ __device__ static constexpr int w_block(int d_h) { return (d_h + 63) / 64 * 8192; }
+  __host__ __device__ static constexpr int misc() { return sizeof(UpBars) + 16 + kRows * (kUpHeld * 4 + 16); }
+  __host__ __device__ static constexpr int total(int d_h) { return a_bytes() + kUpW * w_block(d_h) + misc() + 1024; }
+};
+
+template <int KS>
+__global__ void __launch_bounds__(kUpThreads, 1)
+tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  const int wb = UpSmem::w_block(a.d_h);
+  unsigned char* const s_w = base + UpSmem::a_bytes();
+  UpBars* const bars = (UpBars*)(s_w + kUpW * wb);
+  uint32_t* const s_tmem = (uint32_t*)(bars + 1);
+  volatile int* const s_abort = (volatile int*)(s_tmem + 1);
+  float* const s_wt = (float*)(s_tmem + 4);              // [128][kUpHeld] normalised weights of a row's runs
+  float2* const s_ml = (float2*)(s_wt + kRows * kUpHeld);       // [128] (M, 1 / L)
+  int2* const s_run = (int2*)(s_ml + kRows);             // [128] first run, runs
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int h = blockIdx.y, z = KS > 1 ? (int)cluster_ctarank() : 0;
+  const long long n_rows = (long long)a.B * a.m, r0 = (long long)blockIdx.x * kRows;
+  const int chunks = (a.vw + 63) >> 6, c0 = chunks * z / KS, c1 = chunks * (z + 1) / KS;
+  const int n_w = (a.d_h + 63) >> 6;
+  const uint32_t cols = a.d_h <= 32 ? 32 : a.d_h <= 64 ? 64 : a.d_h <= 128 ? 128 : 256;
+
+  if (tid == 0) {
+    for (int i = 0; i < kUpW; ++i) mbar_init(smem_u32(&bars->w_full[i]), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->done[i]), 1);
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  // W_uv's block of chunk c (the layer's own copy: no kernel writes it)
+  auto load_w = [&](int c) {
+    const uint32_t fb = smem_u32(&bars->w_full[(c - c0) % kUpW]), dst = smem_u32(s_w) + (uint32_t)((c - c0) % kUpW) * wb;
+    mbar_expect_tx(fb, (uint32_t)wb);
+    for (int j = 0; j < n_w; ++j) tma_load_2d(dst + j * 8192, &map_w, h * a.d_h + j * 64, c * 64, fb);
+  };
+  if (tid == 0)
+    for (int c = c0; c < c1 && c < c0 + 2; ++c) load_w(c);
+  ekv_pdl_wait();
+  ekv_pdl_trigger();
+
+  // ---- a row's runs, its largest reference and its sum
+  const int half = h / a.hb, hr = (h - half * a.hb) * a.m;
+  if (tid < kRows) {
+    const long long R = r0 + tid;
+    int2 run = make_int2(0, 0);
+    float M = -1e30f, L = 0.f;
+    const float2* ml = a.part_ml;
+    if (R < n_rows) {
+      const int b = (int)(R / a.m), i = (int)(R - (long long)b * a.m);
+      run.x = __ldcg(a.seq_first + b);
+      run.y = __ldcg(a.seq_first + b + 1) - run.x;
+      ml += ((long long)run.x * a.n_half + half) * kRows + hr + i;
+      for (int k = 0; k < run.y; ++k) M = fmaxf(M, __ldcg(ml + (long long)k * a.n_half * kRows).x);
+      for (int k = 0; k < run.y; ++k) {
+        const float2 x = __ldcg(ml + (long long)k * a.n_half * kRows);
+        L = fmaf(x.y, exp2f(x.x - M), L);
+      }
+    }
+    const float inv = L != 0.f ? 1.f / L : 0.f;          // (nothing seen: a zero row)
+    for (int k = 0; k < kUpHeld; ++k) s_wt[tid * kUpHeld + k] = k < run.y ? exp2f(__ldcg(ml + (long long)k * a.n_half * kRows).x - M) * inv : 0.f;
+    s_ml[tid] = make_float2(M, inv);
+    s_run[tid] = run;
+  }
+  __syncthreads();
+
+  const int col4 = tid & 15, row_t = tid >> 4;           // 4 of a chunk's columns, rows row_t + 16 p
+  const float* src[8];
+  int n_run[8], most = 0;
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const int row = row_t + 16 * p;
+    const long long R = r0 + row;
+    const int2 run = s_run[row];
+    const int i = (int)(R % a.m);
+    n_run[p] = R < n_rows ? run.y : 0;
+    src[p] = a.part_acc + (((long long)run.x * a.n_half + half) * kRows + hr + i) * a.vw + col4 * 4;
+    most = max(most, n_run[p]);
+  }
+  const long long run_pitch = (long long)a.n_half * kRows * a.vw;
+  auto fetch = [&](int c, int k, float4* x) {
+    const bool in = c < c1 && c * 64 + col4 * 4 < a.vw;
+#pragma unroll
+    for (int p = 0; p < 8; ++p)
+      x[p] = in && k < n_run[p] ? __ldcg((const float4*)(src[p] + k * run_pitch + c * 64)) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  const uint32_t idesc = make_idesc(kRows, 16, 0, 1) + ((uint32_t)((a.d_h >> 3) - 2) << 17);
+  constexpr uint32_t hi_sw = desc_hi(1024, 2);
+  bool ok = true;
+  float4 x[8];
+  fetch(c0, 0, x);
+  for (int c = c0; c < c1 && ok; ++c) {
+    const int st = (c - c0) & 1;
+    float4 acc[8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const float w = s_wt[(row_t + 16 * p) * kUpHeld];
+      // (a weight of zero keeps out what a row without a sum holds)
+      acc[p] = w != 0.f ? make_float4(x[p].x * w, x[p].y * w, x[p].z * w, x[p].w * w) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int k = 1; k < most; ++k) {
+      float4 y[8];
+      fetch(c, k, y);
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        const int row = row_t + 16 * p;
+        float w = 0.f;
+        if (k < n_run[p]) {
+          if (k < kUpHeld) {
+            w = s_wt[row * kUpHeld + k];
+          } else {
+            const long long R = r0 + row;
+            w = exp2f(__ldcg(a.part_ml + ((long long)(s_run[row].x + k) * a.n_half + half) * kRows + hr + (int)(R % a.m)).x - s_ml[row].x) * s_ml[row].y;
+          }
+        }
+        if (w != 0.f) {
+          acc[p].x = fmaf(y[p].x, w, acc[p].x); acc[p].y = fmaf(y[p].y, w, acc[p].y);
+          acc[p].z = fmaf(y[p].z, w, acc[p].z); acc[p].w = fmaf(y[p].w, w, acc[p].w);
+        }
+      }
+    }
+    fetch(c + 1, 0, x);                    // in flight while this chunk is laid out and multiplied
+    // the products of chunk c - 2 have read the stage
+    if (c - c0 >= 2) ok = mbar_wait(smem_u32(&bars->done[st]), (uint32_t)(((c - c0) >> 1) - 1) & 1, s_abort, 1);
+    if (tid == 0 && ok && c + 2 < c1) load_w(c + 2);
+    unsigned char* const hi = base + st * 2 * kRows * 128;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const int row = row_t + 16 * p;
+      const bf162 h0 = __floats2bfloat162_rn(acc[p].x, acc[p].y), h1 = __floats2bfloat162_rn(acc[p].z, acc[p].w);
+      const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
+      const bf162 l0 = __floats2bfloat162_rn(acc[p].x - f0.x, acc[p].y - f0.y), l1 = __floats2bfloat162_rn(acc[p].z - f1.x, acc[p].w - f1.y);
+      const int at = row * 128 + (((col4 >> 1) ^ (row & 7)) << 4) + (col4 & 1) * 8;
+      *(uint2*)(hi + at) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
+      *(uint2*)(hi + kRows * 128 + at) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
+    }
+    fence_proxy_async();
+    ok = __syncthreads_and(ok) != 0;
+    if (warp == 0 && ok) {
+      ok = warp_wait(smem_u32(&bars->w_full[(c - c0) % kUpW]), (uint32_t)((c - c0) / kUpW) & 1, s_abort, 2);
+      tc_fence_after();
+      if (ok && elect_one()) {
+        const uint32_t la = desc_lo(smem_u32(hi), 16), lb = desc_lo(smem_u32(s_w) + (uint32_t)((c - c0) % kUpW) * wb, 8192);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          tc_mma_w(tmem, la + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, c != c0 || k != 0);
+          tc_mma_w(tmem, la + (kRows * 128 >> 4) + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, 1);
+        }
+        tc_commit(smem_u32(&bars->done[st]));
+      }
+      __syncwarp();
+    }
+  }
+  // the last products of both stages
+  const int mine = c1 - c0;
+  if (ok && mine >= 2) ok = mbar_wait(smem_u32(&bars->done[mine & 1]), (uint32_t)((mine - 2) >> 1) & 1, s_abort, 3);
+  if (ok && mine >= 1) ok = mbar_wait(smem_u32(&bars->done[(mine - 1) & 1]), (uint32_t)((mine - 1) >> 1) & 1, s_abort, 4);
+  tc_fence_after();
+  ok = __syncthreads_and(ok) != 0;
+
+  const int quarter = warp & 3, part = warp >> 2;        // rows of a warp; two warps share its columns, 8 at a time
+  const int row = quarter * 32 + lane;
+  const long long R = r0 + row;
+  bf16* const dst = a.out + (R * a.n_h + h) * a.d_h;
+  const uint32_t tm = tmem + ((uint32_t)(quarter * 32) << 16);
+  if (KS == 1) {
+    for (int c = part * 8; c < a.d_h && ok; c += 16) {
+      float v[8];
+      tc_ld8(tm + c, v);
+      tc_wait_ld();
+      if (R < n_rows) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *(bf162*)(dst + c + 2 * e) = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+      }
+      __syncwarp();
+    }
+  } else {
+    // every block sends its sums of columns [q w, (q + 1) w) to block q
+    const int w = a.d_h / KS;
+    float* const recv = (float*)base;                    // [source][column][row]
+    cluster_sync_all();                                  // all products are done: the stages are free in every block
+    for (int c = part * 8; c < a.d_h; c += 16) {
+      float v[8];
+      tc_ld8(tm + c, v);
+      tc_wait_ld();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int q = (c + e) / w, k = c + e - q * w;
+        st_cluster_u32(map_to_cta(smem_u32(recv + ((size_t)z * w + k) * kRows + row), (uint32_t)q), __float_as_uint(v[e]));
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();
+    if (R < n_rows && ok) {
+      for (int k = part * 2; k < w; k += 4) {
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int q = 0; q < KS; ++q) {
+          s0 += recv[((size_t)q * w + k) * kRows + row];
+          s1 += recv[((size_t)q * w + k + 1) * kRows + row];
+        }
+        *(bf162*)(dst + z * w + k) = __floats2bfloat162_rn(s0, s1);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (*s_abort) drain_after_abort();
+  if (tid == 0 && *s_abort) ekv_record(a.status, ELITEKV_ERR_TIMEOUT, (int)blockIdx.x | (*s_abort << 16), (int)blockIdx.y);
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+  }
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // rows of a block are whole heads; one block where it holds all of them, else pairs
@@ -910,12 +1225,11 @@ TreeShape tree_shape(const elitekv_layer* L, int m) {
 }
 
 struct TreeCarve {
-  size_t hdr, runs, first, zero, n_zero, stats, pref, cstate, P, qr, ml, acc, slice, cnt, total;
+  size_t hdr, runs, first, zero, n_zero, stats, pref, cstate, P, qr, ml, acc, total;
   size_t max_runs;
 };
 TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   TreeCarve c;
-  const size_t rows = (size_t)m * L->n_h;
   c.max_runs = (size_t)B + s.want;
   const size_t chains = c.max_runs * s.n_rb * s.n_ct;
   size_t o = 0;
@@ -929,10 +1243,9 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * 2 * kRows);
   c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
   c.qr = o;     o = align256(o + sizeof(bf16) * (size_t)B * s.n_rb * s.cg * s.n_rc * kRows * 64);
-  c.ml = o;     o = align256(o + sizeof(float) * 2 * c.max_runs * rows);
-  c.acc = o;    o = align256(o + sizeof(float) * c.max_runs * rows * L->vw);
-  c.slice = o;  o = align256(o + ekv_combine_scratch_bytes(L, B) * m);
-  c.cnt = o;    o = align256(o + sizeof(int32_t) * (size_t)ekv_combine_counters(L, B) * m);
+  const size_t tile_rows = c.max_runs * s.n_rb * s.cg * kRows;
+  c.ml = o;     o = align256(o + sizeof(float2) * tile_rows);
+  c.acc = o;    o = align256(o + sizeof(float) * tile_rows * L->vw);
   c.total = o;
   return c;
 }
@@ -944,6 +1257,26 @@ int make_map_pitch(CUtensorMap* m, const void* ptr, unsigned long long rows, uns
   cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch * sizeof(bf16)};
   cuuint32_t box[2] = {64, box_rows}, estr[2] = {1, 1};
   CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
+}
+// fp32 [rows][cols], box [32][32], 128-byte swizzle
+int make_map_out(CUtensorMap* m, const void* ptr, unsigned long long rows, unsigned long long cols) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return ELITEKV_ERR_CUDA;
+  cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * sizeof(float)};
+  cuuint32_t box[2] = {32, 32}, estr[2] = {1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
+}
+// bf16 [rows][cols / 64][64] with `pitch` elements from row to row, box [chunks][64 rows][64]: whole chunks of 64 columns
+int make_map_chunks(CUtensorMap* m, const void* ptr, unsigned long long rows, unsigned long long cols, unsigned long long pitch, unsigned chunks) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return ELITEKV_ERR_CUDA;
+  cuuint64_t dims[3] = {64, rows, cols / 64}, strides[2] = {pitch * sizeof(bf16), 128};
+  cuuint32_t box[3] = {64, 64, chunks}, estr[3] = {1, 1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
 }
@@ -969,9 +1302,14 @@ size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m) { return tree_car
 
 // Pages of 8 tokens and more: a box of the copy engine is whole 1024-byte groups of the swizzle.  Box coordinates have 32 bits,
 // rope rows whole 16 bytes.
-int ekv_tree_tc_supported(const elitekv_layer* L, const CacheView* cv) {
+int ekv_tree_tc_supported(const elitekv_layer* L, int B, int m, const CacheView* cv) {
+  const TreeShape s = tree_shape(L, m);
+  if (((unsigned long long)B + s.want) * s.n_rb * s.cg * kRows >= (1ull << 31) ||
+      (unsigned long long)B * s.n_rb * s.cg * s.n_rc * kRows >= (1ull << 31) || L->n_h > 65535)
+    return 0;
   if ((L->n_h * L->r) % 4 != 0) return 0;
-  if (TreeSmem<1>::total > L->smem_optin || TreeSmem<2>::total > L->smem_optin) return 0;
+  if (L->d_h % 16 != 0 || L->d_h > 256) return 0;          // the last product's width
+  if (TreeSmem<1>::total > L->smem_optin || TreeSmem<2>::total > L->smem_optin || UpSmem::total(L->d_h) > L->smem_optin) return 0;
   if (cv && cv->page_table && (1 << cv->page_shift) < 8) return 0;
   if (cv && (plane_rows(*cv) >= (1ull << 31) || cv->max_ctx > (1ll << 30))) return 0;
   return 1;
@@ -1006,15 +1344,22 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.v_done = a.ready + kSlots;
   a.chain = a.v_done + kSlots;
   a.part_acc = (float*)(base + w.acc);
-  a.part_ml = (float*)(base + w.ml);
+  a.part_ml = (float2*)(base + w.ml);
   a.hdr = (const int*)(base + w.hdr);
   a.runs = (const int4*)(base + w.runs);
   a.status = L->d_status;
-  CUtensorMap m_q, m_k, m_v, m_p, m_qr, m_r;
+  CUtensorMap m_q, m_k, m_v, m_p, m_qr, m_r, m_ps, m_o, m_w;
+  a.v3 = a.box_v == 64 && L->vw % 64 == 0;
+  const unsigned long long tile_rows = (unsigned long long)w.max_runs * s.n_rb * s.cg * kRows;
   const unsigned long long rows = plane_rows(cv);
   int rc = make_map_queries(&m_q, c.q_abs, c.B, c.m, L->n_h, L->kw, s.hb);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_k, cache->latent, rows, L->kw, L->d_c, a.box_s);
-  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
+  if (rc == ELITEKV_OK)
+    rc = a.v3 ? make_map_chunks(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, 4 / s.cg)
+              : make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
+  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_ps, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, 32);
+  if (rc == ELITEKV_OK) rc = make_map_out(&m_o, a.part_acc, tile_rows, L->vw);
+  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_w, L->d_Wuv, L->vw, (unsigned long long)L->n_h * L->d_h, (unsigned long long)L->n_h * L->d_h, 64);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, kRows);
   // (a layer without rope has neither; the maps are not used)
   m_qr = m_r = m_p;
@@ -1045,10 +1390,8 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   p.seq_first = (int32_t*)(base + w.first);
   p.zero = a.s_cnt;
   p.n_zero = (int)w.n_zero;
-  p.counters = (int32_t*)(base + w.cnt);
-  p.n_counters = ekv_combine_counters(L, c.B) * c.m;
   p.status = L->d_status;
-  const int n_max = p.n_zero > p.n_counters ? p.n_zero : p.n_counters, zero_blocks = (n_max + 1023) / 1024;
+  const int zero_blocks = (p.n_zero + 1023) / 1024;
   p.zero_blocks = zero_blocks < 32 ? zero_blocks : 32;
   const long long qr_blocks = ((long long)c.B * s.n_rb * s.cg * s.n_rc * kRows * 8 + 1023) / 1024;
   EKV_CUDA_OK(ekv_launch_pdl(tree_prep_kernel, dim3((unsigned)(1 + p.zero_blocks + (qr_blocks < 1024 ? qr_blocks : 1024))), dim3(256), 0, st, p));
@@ -1069,18 +1412,49 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    EKV_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, m_q, m_k, m_v, m_p, m_qr, m_r, a));
+    EKV_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, m_q, m_k, m_v, m_p, m_qr, m_r, m_ps, m_o, a));
     return ELITEKV_OK;
   };
   rc = s.cg == 2 ? launch(tree_tc_kernel<2>) : launch(tree_tc_kernel<1>);
   if (rc != ELITEKV_OK) return rc;
   EKV_CUDA_OK(cudaGetLastError());
-  DecodeScratch ws = {};
-  ws.rows = c.m;
-  ws.seq_first = p.seq_first;
-  ws.part_ml = a.part_ml;
-  ws.part_acc = a.part_acc;
-  ws.slice_out = (float*)(base + w.slice);
-  ws.counters = p.counters;
-  return ekv_launch_combine(L, c.B, ws, c.out, st);
+  UpArgs u;
+  u.part_acc = a.part_acc;
+  u.part_ml = a.part_ml;
+  u.seq_first = p.seq_first;
+  u.out = (bf16*)c.out;
+  u.B = c.B;
+  u.m = c.m;
+  u.n_h = L->n_h;
+  u.d_h = L->d_h;
+  u.hb = s.hb;
+  u.n_half = s.n_rb * s.cg;
+  u.vw = L->vw;
+  u.status = L->d_status;
+  // shares of the depth while there are SMs for them, at least two steps each
+  const long long tiles = L->n_h * (((long long)c.B * c.m + kRows - 1) / kRows);
+  const int chunks = (L->vw + 63) / 64;
+  const int ks = tiles * 2 > L->sm_count || chunks < 4 ? 1 : tiles * 4 > L->sm_count || chunks < 8 ? 2 : 4;
+  auto launch_up = [&](auto kern) -> int {
+    const size_t sm = UpSmem::total(L->d_h);
+    EKV_CUDA_OK(ekv_allow_smem(kern, sm));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles / L->n_h), (unsigned)L->n_h, (unsigned)ks);
+    cfg.blockDim = dim3(kUpThreads);
+    cfg.dynamicSmemBytes = sm;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = (unsigned)ks;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    EKV_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, m_w, u));
+    EKV_CUDA_OK(cudaGetLastError());
+    return ELITEKV_OK;
+  };
+  return ks == 4 ? launch_up(tree_up_kernel<4>) : ks == 2 ? launch_up(tree_up_kernel<2>) : launch_up(tree_up_kernel<1>);
 }
