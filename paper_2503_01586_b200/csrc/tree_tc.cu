@@ -44,16 +44,16 @@ namespace {
 constexpr int kRows = 128;              // rows per block
 constexpr int kTile = 256;              // tokens of a score unit, latent columns of a value unit
 constexpr int kPiece = 2048;            // most tokens of a piece
-constexpr int kHalfTiles = kPiece / 128;
+constexpr int kTiles = kPiece / kTile;
 constexpr int kSlots = 64;              // pieces in the ring
 constexpr int kMostAhead = kSlots - 8;  // D at most
 constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 loads cache rows, 3 clears drafted rows, 4-11 epilogue, 12 claims units
-constexpr int kEpiThreads = 256;
-constexpr int kQueue = 2;               // units claimed ahead would be late for those that wait for them
+constexpr int kEpiThreads = 128;         // a group of four epilogue warps
+constexpr int kQueue = 4;               // two units with the epilogue groups, two ahead (more would be late for those that wait for them)
 constexpr int kUnitWords = 16;
 constexpr int kMaxStages = 6;
 constexpr int kABytes = kRows * 128;
-constexpr int kStageBytes = 4096;       // 32 rows of 128 bytes on their way out, per epilogue warp
+constexpr int kOutBytes = 4096;         // rows on their way out, per epilogue warp
 
 enum { kScore = 0, kValue = 1, kStop = 2 };
 
@@ -68,9 +68,9 @@ struct TreeTcArgs {
   int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v, v3;
   float scale_log2e;
   bf16* P;                    // [slot][CG][128][kPiece]
-  float2* stats;              // [slot][CG][2 tiles][128]: (reference, sum) of a row's 128 tokens
+  float2* stats;              // [slot][CG][tiles][128]: (reference, sum) of a row's 256 tokens
   float2* pref;               // [slot][CG][128]: the same of the piece
-  float2* cstate;             // [run][rb][ct][CG][2][128]: of the run so far
+  float2* cstate;             // [run][rb][ct][CG][128]: of the run so far
   int *s_cnt, *ready, *v_done, *chain;
   float* part_acc;            // [run][rb][CG][128][vw]
   float2* part_ml;            // [run][rb][CG][128]
@@ -90,7 +90,7 @@ struct TreeSmem {
   static constexpr int b_bytes = kTile / CG * 128;            // 256 (128) token rows, or 64 tokens of 256 (128) columns
   static constexpr int stage = kABytes + b_bytes;
   static constexpr int n_stages = CG == 2 ? 6 : 4;
-  static constexpr int out = 8 * kStageBytes;
+  static constexpr int out = 8 * kOutBytes;
   static constexpr int misc = sizeof(TreeBars) + kQueue * sizeof(TreeUnit) + kQueue * 16 + 64;
   static constexpr int total = n_stages * stage + out + misc + 1024;
 };
@@ -180,8 +180,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   volatile unsigned long long* const s_nf = (volatile unsigned long long*)(s_unit + kQueue);
   uint32_t* const s_tmem = (uint32_t*)(s_nf + 2 * kQueue);
   volatile int* const s_abort = (volatile int*)(s_tmem + 1);
-  volatile int* const s_verdict = s_abort + 1;      // [2]
-  volatile int* const s_last = s_verdict + 2;
+  volatile int* const s_verdict = s_abort + 1;      // [2 groups][2]
+  volatile int* const s_last = s_verdict + 4;       // [2 groups]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
 
@@ -194,11 +194,11 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars->acc_full[i]), 1);
-      mbar_init(smem_u32(&bars->acc_empty[i]), 8 * CG);
+      mbar_init(smem_u32(&bars->acc_empty[i]), 4 * CG);
     }
     for (int i = 0; i < kQueue; ++i) {
       mbar_init(smem_u32(&bars->q_full[i]), kUnitWords);
-      mbar_init(smem_u32(&bars->q_empty[i]), 1 + 11 * CG);
+      mbar_init(smem_u32(&bars->q_empty[i]), 1 + 7 * CG);
     }
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -508,6 +508,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       wv.r = ws.r;
       wv.r2 = ws.r2;
       int first = 0, j = 0;                    // first unit of block j
+      bool stopped = false;
       for (;; ++q_pos) {
         if (!warp_wait_cluster(smem_u32(&bars->q_empty[q_slot()]), q_parity() ^ 1, s_abort, 11)) break;
         int unit = 0;
@@ -557,33 +558,37 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           }
         }
         __syncwarp();
-        if (stop) break;
+        if (stop && stopped) break;            // once for each epilogue group
+        stopped = stop;
       }
     }
   } else {
-    // ============================================================== epilogue: thread = (row, half of the columns)
-    const int quarter = warp & 3, ch = (warp - 4) >> 2, r = quarter * 32 + lane;
-    const bool leader = threadIdx.x == 128;
-    const uint32_t tm_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ch * 128);
+    // ============================================================== epilogue: thread = row; two groups of four warps
+    // Group g has the units at even (odd) places and their accumulator, so that the waits of one group's unit (rows on
+    // their way to memory, counters) pass while the other computes.
+    const int group_id = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const bool leader = (threadIdx.x & 127) == 0;
+    const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group_id * kTile);
     const int hl = r / a.m, i = r - hl * a.m;
-    unsigned char* const s_out = base + NST * SM::stage + (warp - 4) * kStageBytes;      // 32 rows of 128 bytes, swizzled
-    const uint32_t out_row = smem_u32(s_out) + lane * 128;
-    // 16 bytes of this lane's row
-    auto put = [&](int j, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out_row + ((j ^ (lane & 7)) << 4)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+    volatile int* const verdict = s_verdict + 2 * group_id;
+    volatile int* const last = s_last + group_id;
+    // rows on their way out: two boxes of 32 rows x 64 bytes per warp (64-byte swizzle)
+    const uint32_t out_box = smem_u32(base + NST * SM::stage + (warp - 4) * kOutBytes);
+    auto put = [&](int box, int j, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {       // 16 bytes of this lane's row
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                   ::"r"(out_box + box * (kOutBytes / 2) + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
     };
-    // the warp's box is free again / is full
-    auto out_free = [&]() {
-      if (lane == 0) bulk_wait_group_read<0>();
+    auto out_free = [&]() {                     // the box of the store before the last has been read
+      if (lane == 0) bulk_wait_group_read<1>();
       __syncwarp();
     };
     unsigned turn = 0;
     // the leader looks, everybody gets its verdict
     auto group = [&](auto probe) -> bool {
-      volatile int* const word = s_verdict + (turn & 1u);
+      volatile int* const word = verdict + (turn & 1u);
       ++turn;
       if (leader) *word = probe() ? 1 : 0;
-      named_bar_sync(2, kEpiThreads);
+      named_bar_sync(2 + group_id, kEpiThreads);
       return *word != 0;
     };
     auto group_bar = [&](uint32_t bar, uint32_t parity, int why) -> bool {
@@ -598,14 +603,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       if (ok) (void)mbar_try_wait_cluster(bar, parity);
       return ok;
     };
-    for (;; ++q_pos) {
+    for (q_pos = group_id;; q_pos += 2) {
       if (!group_bar(smem_u32(&bars->q_full[q_slot()]), q_parity(), 12)) break;
       const volatile TreeUnit* u = s_unit + q_slot();
       const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, gen = u->gen, n = u->n;
       const int nodes = u->nodes, run = u->run, k_run = u->k, prefix = n - nodes;
       if (type == kStop) break;
-      const unsigned buf = q_pos & 1;
-      const uint32_t tm = tm_row + buf * kTile, acc_bar = smem_u32(&bars->acc_full[buf]), acc_par = (q_pos >> 1) & 1;
+      const uint32_t acc_bar = smem_u32(&bars->acc_full[group_id]), acc_par = (q_pos >> 1) & 1;
       const int h = (rb * CG + (int)rank) * a.hb + hl;
       const bool real = hl < a.hb && h < a.n_h, active = real && i < nodes;
       const unsigned long long mask = active ? a.mask[(long long)b * a.m + i] : 0ull;
@@ -614,18 +618,18 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          const uint32_t bar = smem_u32(&bars->acc_empty[buf]);
+          const uint32_t bar = smem_u32(&bars->acc_empty[group_id]);
           if (CG == 2) mbar_arrive_cluster(map_to_cta(bar, 0)); else mbar_arrive(bar);
         }
       };
       if (type == kScore) {
-        const int t0 = tok0 + idx * kTile + ch * 128;              // this thread's 128 tokens
+        const int t0 = tok0 + idx * kTile;
         // the slot's last piece is read to the end
         if (gen > 0 && !group([&]() { return poll_global(a.v_done + slot, gen * a.n_ct * CG, s_abort, 13); })) break;
         if (!group_bar(acc_bar, acc_par, 14)) break;
         tc_fence_after();
         // which of 32 tokens the row sees; tiles of committed tokens alone skip it
-        const bool all = t0 + 128 <= prefix;
+        const bool all = t0 + kTile <= prefix;
         auto seen_bits = [&](int t) -> unsigned {                  // tokens t .. t + 31
           if (t + 32 <= prefix) return 0xffffffffu;
           const int d = prefix - t;                                // committed ones in front: d of them
@@ -637,25 +641,17 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         float ref = 0.f, sum = 0.f;
         for (bool again = false;;) {
           float top = -INFINITY, sum4[4] = {0.f, 0.f, 0.f, 0.f};
-          float v[2][32];
-          tc_ld32(tm, v[0]);
-#pragma unroll
-          for (int cc = 0; cc < 4; ++cc) {
-            float* const x = v[cc & 1];
-            tc_wait_ld();
-            if (cc < 3) tc_ld32(tm + (cc + 1) * 32, v[(cc + 1) & 1]);
+          auto chunk = [&](int cc, float* x) {                     // 32 tokens
             if (!all) {
               const unsigned bits = seen_bits(t0 + cc * 32);
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] = bits >> e & 1 ? x[e] : -INFINITY;
             }
-            if (!again) {
-              float t4[4] = {x[0], x[1], x[2], x[3]};
+            float t4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-              for (int e = 4; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], x[e]);
-              top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
-            }
-            if ((cc & 1) == 0) out_free();
+            for (int e = 4; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], x[e]);
+            top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+            out_free();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
               uint32_t w[4];
@@ -666,16 +662,25 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 sum4[2 * (e & 1)] += __uint_as_float(w[e] << 16);
                 sum4[2 * (e & 1) + 1] += __uint_as_float(w[e] & 0xffff0000u);
               }
-              put((cc & 1) * 4 + g, w[0], w[1], w[2], w[3]);
+              put(cc & 1, g, w[0], w[1], w[2], w[3]);
             }
-            if (cc & 1) {
-              fence_proxy_async();
-              __syncwarp();
-              if (lane == 0) {
-                tma_store_2d(&map_ps, idx * kTile + ch * 128 + (cc >> 1) * 64, (int)half * kRows + quarter * 32, smem_u32(s_out));
-                bulk_commit_group();
-              }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_2d(&map_ps, idx * kTile + cc * 32, (int)half * kRows + quarter * 32, out_box + (cc & 1) * (kOutBytes / 2));
+              bulk_commit_group();
             }
+          };
+          float v0[32], v1[32];
+          tc_ld32(tm, v0);
+#pragma unroll 1
+          for (int cc = 0; cc < kTile / 32; cc += 2) {
+            tc_wait_ld();
+            tc_ld32(tm + (cc + 1) * 32, v1);
+            chunk(cc, v0);
+            tc_wait_ld();
+            if (cc + 2 < kTile / 32) tc_ld32(tm + (cc + 2) * 32, v0);
+            chunk(cc + 1, v1);
           }
           sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
           if (again) break;
@@ -689,52 +694,49 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
         if (!active) sum = 0.f;
         acc_done();
-        a.stats[(half * kHalfTiles + idx * 2 + ch) * kRows + r] = make_float2(ref, sum);
+        a.stats[(half * kTiles + idx) * kRows + r] = make_float2(ref, sum);
         if (lane == 0) {
           bulk_wait_group_all();             // the rows are in memory
           fence_proxy_all();
         }
         __threadfence();
-        named_bar_sync(2, kEpiThreads);
+        named_bar_sync(2 + group_id, kEpiThreads);
+        const int tiles = (len + kTile - 1) / kTile;
         if (leader) {
-          const int tiles = (len + kTile - 1) / kTile;
           const int before = atomicAdd(a.s_cnt + half, 1);
           __threadfence();
-          *s_last = before == tiles - 1;
+          *last = before == tiles - 1;
         }
-        named_bar_sync(2, kEpiThreads);
-        if (*s_last) {
+        named_bar_sync(2 + group_id, kEpiThreads);
+        if (*last) {
           // the piece's rows agree on a reference
-          const int tiles = 2 * ((len + kTile - 1) / kTile);
-          if (ch == 0) {
-            const float2* const st = a.stats + half * kHalfTiles * kRows + r;
-            float m_ref = -1e30f, total = 0.f;
-#pragma unroll 4
-            for (int t = 0; t < tiles; ++t) {
-              const float2 x = __ldcg(st + t * kRows);
-              if (x.y != 0.f) m_ref = fmaxf(m_ref, x.x);
-            }
-#pragma unroll 4
-            for (int t = 0; t < tiles; ++t) {
-              const float2 x = __ldcg(st + t * kRows);
-              if (x.y == 0.f) continue;
-              const float f = x.x == m_ref ? 1.f : exp2f(x.x - m_ref);
-              total = fmaf(x.y, f, total);
-              if (f != 1.f && real) {
-                uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * 128);
+          const float2* const st = a.stats + half * kTiles * kRows + r;
+          float m_ref = -1e30f, total = 0.f;
+          float2 x[kTiles];
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) x[t] = t < tiles ? __ldcg(st + t * kRows) : make_float2(0.f, 0.f);
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t)
+            if (x[t].y != 0.f) m_ref = fmaxf(m_ref, x[t].x);
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            if (x[t].y == 0.f) continue;
+            const float f = x[t].x == m_ref ? 1.f : exp2f(x[t].x - m_ref);
+            total = fmaf(x[t].y, f, total);
+            if (f != 1.f && real) {
+              uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * kTile);
 #pragma unroll 1
-                for (int e = 0; e < 64; ++e) {
-                  const uint32_t w = __ldcg(pr + e);
-                  const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
-                  pr[e] = *(const uint32_t*)&y;
-                }
+              for (int e = 0; e < kTile / 2; ++e) {
+                const uint32_t w = __ldcg(pr + e);
+                const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
+                pr[e] = *(const uint32_t*)&y;
               }
             }
-            a.pref[half * kRows + r] = make_float2(m_ref, total);
           }
+          a.pref[half * kRows + r] = make_float2(m_ref, total);
           fence_proxy_all();
           __threadfence();
-          named_bar_sync(2, kEpiThreads);
+          named_bar_sync(2 + group_id, kEpiThreads);
           if (leader) {
             a.s_cnt[half] = 0;
             add_release(a.ready + slot, 1);
@@ -747,7 +749,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         // the piece before in the run is in the partial result
         if (k_run > 0 && !group([&]() { return poll_global(a.chain + ci, k_run * CG, s_abort, 15); })) break;
         const float2 mine = __ldcg(a.pref + half * kRows + r);
-        float2* const state = a.cstate + ((ci * CG + rank) * 2 + ch) * kRows + r;
+        float2* const state = a.cstate + (ci * CG + rank) * kRows + r;
         const long long tile_row = (((long long)run * a.n_rb + rb) * CG + rank) * kRows;      // of the block's rows in the partial result
         float2 now = mine;
         float f_old = 1.f, f_new = 1.f;
@@ -765,40 +767,50 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const bool none = mine.y == 0.f;
         const bool scaled = __any_sync(0xffffffffu, f_old != 1.f);
         *state = now;
-        if (idx == 0 && ch == 0) a.part_ml[tile_row + r] = now;
-        const int c0 = idx * kTile + ch * 128;
-        float v[2][32];
-        tc_ld32(tm, v[0]);
-#pragma unroll
-        for (int cc = 0; cc < 4; ++cc) {
-          float* const x = v[cc & 1];
-          tc_wait_ld();
-          if (cc < 3) tc_ld32(tm + (cc + 1) * 32, v[(cc + 1) & 1]);
-          const int col = c0 + cc * 32;
-          if (col >= a.vw) continue;                      // (the same for the whole warp)
+        if (idx == 0) a.part_ml[tile_row + r] = now;
+        auto chunk = [&](int cc, float* x) {              // 32 columns
+          const int col = idx * kTile + cc * 32;
+          if (col >= a.vw) return;                        // (the same for the whole warp)
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = spoiled ? __uint_as_float(0x7fffffffu) : none ? 0.f : x[e] * f_new;
           if (scaled) {                                   // references moved: what is there is scaled by its reader
             const float* const o = a.part_acc + (tile_row + r) * a.vw + col;
+#pragma unroll
             for (int e = 0; e < 32; e += 4)
               if (col + e < a.vw) {
                 const float4 y = __ldcg((const float4*)(o + e));
-#pragma unroll
-                for (int z = 0; z < 32; z += 4)
-                  if (z == e) { x[z] += y.x * f_old; x[z + 1] += y.y * f_old; x[z + 2] += y.z * f_old; x[z + 3] += y.w * f_old; }
+                x[e] += y.x * f_old; x[e + 1] += y.y * f_old; x[e + 2] += y.z * f_old; x[e + 3] += y.w * f_old;
               }
           }
-          out_free();
 #pragma unroll
-          for (int g = 0; g < 8; ++g)
-            put(g, __float_as_uint(x[4 * g]), __float_as_uint(x[4 * g + 1]), __float_as_uint(x[4 * g + 2]), __float_as_uint(x[4 * g + 3]));
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) {
-            if (k_run == 0 || scaled) tma_store_2d(&map_o, col, (int)(tile_row + quarter * 32), smem_u32(s_out));
-            else tma_add_2d(&map_o, col, (int)(tile_row + quarter * 32), smem_u32(s_out));
-            bulk_commit_group();
+          for (int box = 0; box < 2; ++box) {             // 16 columns each
+            if (col + box * 16 >= a.vw) continue;
+            out_free();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const float* y = x + box * 16 + 4 * g;
+              put(box, g, __float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              const uint32_t from = out_box + box * (kOutBytes / 2);
+              if (k_run == 0 || scaled) tma_store_2d(&map_o, col + box * 16, (int)(tile_row + quarter * 32), from);
+              else tma_add_2d(&map_o, col + box * 16, (int)(tile_row + quarter * 32), from);
+              bulk_commit_group();
+            }
           }
+        };
+        float v0[32], v1[32];
+        tc_ld32(tm, v0);
+#pragma unroll 1
+        for (int cc = 0; cc < kTile / 32; cc += 2) {
+          tc_wait_ld();
+          tc_ld32(tm + (cc + 1) * 32, v1);
+          chunk(cc, v0);
+          tc_wait_ld();
+          if (cc + 2 < kTile / 32) tc_ld32(tm + (cc + 2) * 32, v0);
+          chunk(cc + 1, v1);
         }
         acc_done();
         if (lane == 0) {
@@ -806,7 +818,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           fence_proxy_all();
         }
         __threadfence();
-        named_bar_sync(2, kEpiThreads);
+        named_bar_sync(2 + group_id, kEpiThreads);
         if (leader) {
           add_release(a.chain + ci, 1);
           add_release(a.v_done + slot, 1);
@@ -979,7 +991,7 @@ struct UpSmem {
   __host__ __device__ static constexpr int total(int d_h) { return a_bytes() + kUpW * w_block(d_h) + misc() + 1024; }
 };
 
-template <int KS>
+template <int KS, int G>
 __global__ void __launch_bounds__(kUpThreads, 1)
 tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   extern __shared__ unsigned char smem_raw[];
@@ -1050,48 +1062,52 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   }
   __syncthreads();
 
-  const int col4 = tid & 15, row_t = tid >> 4;           // 4 of a chunk's columns, rows row_t + 16 p
-  const float* src[8];
-  int n_run[8], most = 0;
+  // 4 of a chunk's columns of the rows row_t + 16 q; G: calls of few rows have G runs of a row fetched at once
+  constexpr int kQ = 8 / G;
+  const int col4 = tid & 15, row_t = tid >> 4;
+  const float* src[kQ];
+  int n_run[kQ], most = 0;
 #pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    const int row = row_t + 16 * p;
+  for (int q = 0; q < kQ; ++q) {
+    const int row = row_t + 16 * q;
     const long long R = r0 + row;
     const int2 run = s_run[row];
     const int i = (int)(R % a.m);
-    n_run[p] = R < n_rows ? run.y : 0;
-    src[p] = a.part_acc + (((long long)run.x * a.n_half + half) * kRows + hr + i) * a.vw + col4 * 4;
-    most = max(most, n_run[p]);
+    n_run[q] = R < n_rows ? run.y : 0;
+    src[q] = a.part_acc + (((long long)run.x * a.n_half + half) * kRows + hr + i) * a.vw + col4 * 4;
+    most = max(most, n_run[q]);
   }
   const long long run_pitch = (long long)a.n_half * kRows * a.vw;
-  auto fetch = [&](int c, int k, float4* x) {
+  auto fetch = [&](int c, int k0, float4* x) {           // runs k0 .. k0 + G - 1 of chunk c
     const bool in = c < c1 && c * 64 + col4 * 4 < a.vw;
 #pragma unroll
-    for (int p = 0; p < 8; ++p)
-      x[p] = in && k < n_run[p] ? __ldcg((const float4*)(src[p] + k * run_pitch + c * 64)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < 8; ++p) {
+      const int q = p / G, k = k0 + p % G;
+      x[p] = in && k < n_run[q] ? __ldcg((const float4*)(src[q] + k * run_pitch + c * 64)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
   };
   const uint32_t idesc = make_idesc(kRows, 16, 0, 1) + ((uint32_t)((a.d_h >> 3) - 2) << 17);
   constexpr uint32_t hi_sw = desc_hi(1024, 2);
   bool ok = true;
-  float4 x[8];
-  fetch(c0, 0, x);
-  for (int c = c0; c < c1 && ok; ++c) {
+  // one chunk: its first run's rows are in x, those of chunk c + 2 are requested
+  auto step = [&](int c, float4* x) {
     const int st = (c - c0) & 1;
     float4 acc[8];
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-      const float w = s_wt[(row_t + 16 * p) * kUpHeld];
+      const float w = s_wt[(row_t + 16 * (p / G)) * kUpHeld + p % G];
       // (a weight of zero keeps out what a row without a sum holds)
       acc[p] = w != 0.f ? make_float4(x[p].x * w, x[p].y * w, x[p].z * w, x[p].w * w) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int k = 1; k < most; ++k) {
+    fetch(c + 2, 0, x);                    // in flight while this chunk is laid out and multiplied
+    for (int k0 = G; k0 < most; k0 += G) {
       float4 y[8];
-      fetch(c, k, y);
+      fetch(c, k0, y);
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
-        const int row = row_t + 16 * p;
+        const int row = row_t + 16 * (p / G), k = k0 + p % G;
         float w = 0.f;
-        if (k < n_run[p]) {
+        if (k < n_run[p / G]) {
           if (k < kUpHeld) {
             w = s_wt[row * kUpHeld + k];
           } else {
@@ -1105,17 +1121,19 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
         }
       }
     }
-    fetch(c + 1, 0, x);                    // in flight while this chunk is laid out and multiplied
     // the products of chunk c - 2 have read the stage
     if (c - c0 >= 2) ok = mbar_wait(smem_u32(&bars->done[st]), (uint32_t)(((c - c0) >> 1) - 1) & 1, s_abort, 1);
     if (tid == 0 && ok && c + 2 < c1) load_w(c + 2);
     unsigned char* const hi = base + st * 2 * kRows * 128;
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const int row = row_t + 16 * p;
-      const bf162 h0 = __floats2bfloat162_rn(acc[p].x, acc[p].y), h1 = __floats2bfloat162_rn(acc[p].z, acc[p].w);
+    for (int q = 0; q < 8 / G; ++q) {
+      const int row = row_t + 16 * q;
+      float4 v = acc[q * G];
+#pragma unroll
+      for (int g = 1; g < G; ++g) { v.x += acc[q * G + g].x; v.y += acc[q * G + g].y; v.z += acc[q * G + g].z; v.w += acc[q * G + g].w; }
+      const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
       const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
-      const bf162 l0 = __floats2bfloat162_rn(acc[p].x - f0.x, acc[p].y - f0.y), l1 = __floats2bfloat162_rn(acc[p].z - f1.x, acc[p].w - f1.y);
+      const bf162 l0 = __floats2bfloat162_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2bfloat162_rn(v.z - f1.x, v.w - f1.y);
       const int at = row * 128 + (((col4 >> 1) ^ (row & 7)) << 4) + (col4 & 1) * 8;
       *(uint2*)(hi + at) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
       *(uint2*)(hi + kRows * 128 + at) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
@@ -1136,6 +1154,16 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
       }
       __syncwarp();
     }
+  };
+  float4 x0[8], x1[8];
+  fetch(c0, 0, x0);
+  fetch(c0 + 1, 0, x1);
+#pragma unroll 1
+  for (int c = c0; c < c1; c += 2) {
+    step(c, x0);
+    if (!ok || c + 1 >= c1) break;
+    step(c + 1, x1);
+    if (!ok) break;
   }
   // the last products of both stages
   const int mine = c1 - c0;
@@ -1238,9 +1266,9 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.first = o;  o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
   c.n_zero = (size_t)kSlots * (s.cg + 2) + chains;
   c.zero = o;   o = align256(o + sizeof(int) * c.n_zero);
-  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * kHalfTiles * kRows);
+  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * kTiles * kRows);
   c.pref = o;   o = align256(o + sizeof(float2) * kSlots * s.cg * kRows);
-  c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * 2 * kRows);
+  c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * kRows);
   c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
   c.qr = o;     o = align256(o + sizeof(bf16) * (size_t)B * s.n_rb * s.cg * s.n_rc * kRows * 64);
   const size_t tile_rows = c.max_runs * s.n_rb * s.cg * kRows;
@@ -1260,14 +1288,14 @@ int make_map_pitch(CUtensorMap* m, const void* ptr, unsigned long long rows, uns
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
 }
-// fp32 [rows][cols], box [32][32], 128-byte swizzle
-int make_map_out(CUtensorMap* m, const void* ptr, unsigned long long rows, unsigned long long cols) {
+// [rows][cols], box of 32 rows x 64 bytes, 64-byte swizzle: what the epilogue warps write
+int make_map_box(CUtensorMap* m, CUtensorMapDataType type, const void* ptr, unsigned long long rows, unsigned long long cols, unsigned size) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return ELITEKV_ERR_CUDA;
-  cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * sizeof(float)};
-  cuuint32_t box[2] = {32, 32}, estr[2] = {1, 1};
-  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * size};
+  cuuint32_t box[2] = {64 / size, 32}, estr[2] = {1, 1};
+  CUresult r = fn(m, type, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
 }
 // bf16 [rows][cols / 64][64] with `pitch` elements from row to row, box [chunks][64 rows][64]: whole chunks of 64 columns
@@ -1357,8 +1385,8 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   if (rc == ELITEKV_OK)
     rc = a.v3 ? make_map_chunks(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, 4 / s.cg)
               : make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
-  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_ps, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, 32);
-  if (rc == ELITEKV_OK) rc = make_map_out(&m_o, a.part_acc, tile_rows, L->vw);
+  if (rc == ELITEKV_OK) rc = make_map_box(&m_ps, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, 2);
+  if (rc == ELITEKV_OK) rc = make_map_box(&m_o, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a.part_acc, tile_rows, L->vw, 4);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_w, L->d_Wuv, L->vw, (unsigned long long)L->n_h * L->d_h, (unsigned long long)L->n_h * L->d_h, 64);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, kRows);
   // (a layer without rope has neither; the maps are not used)
@@ -1456,5 +1484,8 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
     EKV_CUDA_OK(cudaGetLastError());
     return ELITEKV_OK;
   };
-  return ks == 4 ? launch_up(tree_up_kernel<4>) : ks == 2 ? launch_up(tree_up_kernel<2>) : launch_up(tree_up_kernel<1>);
+  const long long up_rows = (long long)c.B * c.m;         // of the only row block, where there is one
+  if (up_rows <= 16) return ks == 4 ? launch_up(tree_up_kernel<4, 8>) : ks == 2 ? launch_up(tree_up_kernel<2, 8>) : launch_up(tree_up_kernel<1, 8>);
+  if (up_rows <= 64) return ks == 4 ? launch_up(tree_up_kernel<4, 2>) : ks == 2 ? launch_up(tree_up_kernel<2, 2>) : launch_up(tree_up_kernel<1, 2>);
+  return ks == 4 ? launch_up(tree_up_kernel<4, 1>) : ks == 2 ? launch_up(tree_up_kernel<2, 1>) : launch_up(tree_up_kernel<1, 1>);
 }
