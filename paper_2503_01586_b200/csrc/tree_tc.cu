@@ -50,7 +50,7 @@ constexpr int kMostAhead = kSlots - 8;  // D at most
 constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 loads cache rows, 3 clears drafted rows, 4-11 epilogue, 12 claims units
 constexpr int kEpiThreads = 128;         // a group of four epilogue warps
 constexpr int kQueue = 4;               // two units with the epilogue groups, two ahead (more would be late for those that wait for them)
-constexpr int kUnitWords = 16;
+constexpr int kLead = 6;                // steps before a unit's last load at which the next unit is claimed
 constexpr int kMaxStages = 6;
 constexpr int kABytes = kRows * 128;
 constexpr int kOutBytes = 4096;         // rows on their way out, per epilogue warp
@@ -58,9 +58,8 @@ constexpr int kOutBytes = 4096;         // rows on their way out, per epilogue w
 enum { kScore = 0, kValue = 1, kStop = 2 };
 
 struct TreeUnit {
-  int type, b, rb, tok0, len, idx, slot, gen, n, nodes, run, k, pad[4];
+  int type, b, rb, tok0, len, idx, slot, gen, n, nodes, run, k, pad[4];      // 48 bytes are published
 };
-static_assert(sizeof(TreeUnit) == kUnitWords * 4, "published word by word");
 
 struct TreeTcArgs {
   CacheView cv;
@@ -75,14 +74,14 @@ struct TreeTcArgs {
   float* part_acc;            // [run][rb][CG][128][vw]
   float2* part_ml;            // [run][rb][CG][128]
   const int* hdr;             // [0] claim counter, [1] runs, [2] pieces (row blocks included), [3] D
-  const int4* runs;           // [run][2]: (b, first token, tokens, pieces), (n, nodes, ., .)
+  const int4* runs;           // [run][2], by pieces: (b, first token, tokens, pieces), (n, nodes, run, .)
   int32_t* status;
 };
 
-struct __align__(8) TreeBars {
+struct __align__(16) TreeBars {        // (units behind it are written 16 bytes at a time)
   uint64_t full[kMaxStages], empty[kMaxStages], spec[kMaxStages], fixed[kMaxStages];
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t q_full[kQueue], q_empty[kQueue];
+  uint64_t q_full[kQueue], q_empty[kQueue], go;
 };
 
 template <int CG>
@@ -142,25 +141,27 @@ __device__ __forceinline__ long long tree_row(const CacheView& cv, int b, int t,
 __host__ __device__ __forceinline__ int tree_rope_col(int h0, int r2) { return h0 * r2 & ~7; }
 
 // The list of units, walked forward: block j of the list holds the score units of piece j and the value units of
-// piece j - D.  A piece walker stands on one piece (run, k-th piece of the run, row block).
+// piece j - D.  Pieces are ordered by their place in their run, then by run, then by row block, so that the pieces of a
+// run, which add into one partial result in turn, are far apart.  The runs are sorted by their number of pieces: those with
+// a k-th piece are the list's first (up to kBins, from where on the list is searched).
+constexpr int kBins = 256;
 struct PieceWalk {
-  int p, run, k, rb;
-  int4 r, r2;
+  int p, at, k, rb;           // piece; run (place in the list), piece of the run, row block
+  int4 r, r2;                 // (b, first token, tokens, pieces), (n, nodes, run, .)
 };
-__device__ __forceinline__ void walk_load(PieceWalk& w, const TreeTcArgs& a, int n_runs) {
-  if (w.run < n_runs) {
-    w.r = __ldcg(a.runs + 2 * w.run);
-    w.r2 = __ldcg(a.runs + 2 * w.run + 1);
-  }
+__device__ __forceinline__ void walk_load(PieceWalk& w, const TreeTcArgs& a) {
+  w.r = a.runs[2 * w.at];
+  w.r2 = a.runs[2 * w.at + 1];
 }
-__device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int n_runs) {
-  ++w.p;
+__device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int n_runs, int n_pieces) {
+  if (++w.p >= n_pieces) return;
   if (++w.rb < a.n_rb) return;
   w.rb = 0;
-  if (++w.k < w.r.w) return;
-  w.k = 0;
-  ++w.run;
-  walk_load(w, a, n_runs);
+  do {
+    if (++w.at >= n_runs) { w.at = 0; ++w.k; }
+    walk_load(w, a);
+    if (w.r.w <= w.k && w.r.w < kBins) { w.at = 0; ++w.k; walk_load(w, a); }
+  } while (w.r.w <= w.k);
 }
 __device__ __forceinline__ int walk_len(const PieceWalk& w) { return min(kPiece, w.r.z - w.k * kPiece); }
 
@@ -197,9 +198,10 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       mbar_init(smem_u32(&bars->acc_empty[i]), 4 * CG);
     }
     for (int i = 0; i < kQueue; ++i) {
-      mbar_init(smem_u32(&bars->q_full[i]), kUnitWords);
+      mbar_init(smem_u32(&bars->q_full[i]), 1);
       mbar_init(smem_u32(&bars->q_empty[i]), 1 + 7 * CG);
     }
+    mbar_init(smem_u32(&bars->go), 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
@@ -256,6 +258,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage);
           const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
           const bool lat = kc < nkl;
+          if (kc == max(nkc - kLead, 0) && rank == 0 && lane == 0) mbar_arrive(smem_u32(&bars->go));
+          __syncwarp();
           if (elect_one()) {
             if (rank == 0) mbar_expect_tx(fb, lat ? bytes_l : CG * kABytes + bytes_b);
             if (lat) {
@@ -283,6 +287,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           if (!ok) break;
           const uint32_t fb = smem_u32(&bars->full[st]), dst = smem_u32(base + st * SM::stage);
           const uint32_t cfb = CG == 2 ? map_to_cta(fb, 0) : fb;
+          if (ks == max(ks_n - kLead, 0) && rank == 0 && lane == 0) mbar_arrive(smem_u32(&bars->go));
+          __syncwarp();
           if (elect_one()) {
             if (rank == 0) mbar_expect_tx(fb, (uint32_t)(CG * kABytes + (special ? 0 : ch_all * boxes * bv * 128)));
             if (CG == 2) tma_load_2d_pair(dst, &map_p, ks * 64, y, cfb); else tma_load_2d(dst, &map_p, ks * 64, y, cfb);
@@ -503,13 +509,17 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     // ============================================================== units (the first block's warp, for both)
     if (rank == 0) {
       const int n_runs = __ldcg(a.hdr + 1), n_pieces = __ldcg(a.hdr + 2), ahead = __ldcg(a.hdr + 3);
-      PieceWalk ws{0, 0, 0, 0, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)}, wv = ws;
-      walk_load(ws, a, n_runs);
-      wv.r = ws.r;
-      wv.r2 = ws.r2;
-      int first = 0, j = 0;                    // first unit of block j
+      // (the list is read over and over: brought into L1 once)
+      int warm = 0;
+      for (int k = lane * 4; k < n_runs; k += 128) warm |= a.runs[2 * k].x;
+      PieceWalk ws{0, 0, 0, 0, make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+      if (n_runs > 0) walk_load(ws, a);
+      PieceWalk wv = ws;
+      int first = warm < 0 ? 1 : 0, j = 0;     // first unit of block j (no sequence is negative)
       bool stopped = false;
       for (;; ++q_pos) {
+        // claimed late: a unit that waits here while others depend on it holds them up
+        if (q_pos > 0 && !stopped && !warp_wait(smem_u32(&bars->go), (q_pos - 1) & 1, s_abort, 20)) break;
         if (!warp_wait_cluster(smem_u32(&bars->q_empty[q_slot()]), q_parity() ^ 1, s_abort, 11)) break;
         int unit = 0;
         if (lane == 0) unit = atomicAdd((int*)a.hdr, 1);
@@ -522,40 +532,23 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           stop = j >= n_pieces + ahead;
           if (stop || unit < first + n_s + n_v) break;
           first += n_s + n_v;
-          if (j < n_pieces) walk_next(ws, a, n_runs);
-          if (j >= ahead) walk_next(wv, a, n_runs);
+          if (j < n_pieces) walk_next(ws, a, n_runs, n_pieces);
+          if (j >= ahead) walk_next(wv, a, n_runs, n_pieces);
           ++j;
         }
         const int at = unit - first;
         const bool score = at < n_s;
         const PieceWalk& w = score ? ws : wv;
-        int word = 0;
-        switch (lane) {
-          case 0: word = stop ? kStop : score ? kScore : kValue; break;
-          case 1: word = w.r.x; break;
-          case 2: word = w.rb; break;
-          case 3: word = w.r.y + w.k * kPiece; break;
-          case 4: word = walk_len(w); break;
-          case 5: word = score ? at : at - n_s; break;
-          case 6: word = w.p % kSlots; break;
-          case 7: word = w.p / kSlots; break;
-          case 8: word = w.r2.x; break;
-          case 9: word = w.r2.y; break;
-          case 10: word = w.run; break;
-          case 11: word = w.k; break;
-        }
-        if (lane < kUnitWords) {
-          const uint32_t to = smem_u32((const void*)(s_unit + q_slot())) + 4 * lane, bar = smem_u32(&bars->q_full[q_slot()]);
-          if (CG == 2) {
+        int x, y, z, t;                        // 16 bytes of the unit per lane
+        if (lane == 0) { x = stop ? kStop : score ? kScore : kValue; y = w.r.x; z = w.rb; t = w.r.y + w.k * kPiece; }
+        else if (lane == 1) { x = walk_len(w); y = score ? at : at - n_s; z = w.p % kSlots; t = w.p / kSlots; }
+        else { x = w.r2.x; y = w.r2.y; z = w.r2.z; t = w.k; }
+        const uint32_t to = smem_u32((const void*)(s_unit + q_slot())) + 16 * lane, bar = smem_u32(&bars->q_full[q_slot()]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              st_cluster_u32(map_to_cta(to, c), (uint32_t)word);
-              mbar_arrive_cluster(map_to_cta(bar, c));
-            }
-          } else {
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(word) : "memory");
-            mbar_arrive(bar);
-          }
+        for (int c = 0; c < CG; ++c) {
+          const uint32_t cbar = map_to_cta(bar, c);
+          if (lane == 0) mbar_expect_tx_cluster(cbar, 48);
+          if (lane < 3) st_async_v4(map_to_cta(to, c), (uint32_t)x, (uint32_t)y, (uint32_t)z, (uint32_t)t, cbar);
         }
         __syncwarp();
         if (stop && stopped) break;            // once for each epilogue group
@@ -891,6 +884,7 @@ tree_prep_kernel(const TreePrepArgs a) {
   }
   __shared__ long long s_sum[8];
   __shared__ int s_cnt[3][8];
+  __shared__ int s_bin[kBins + 1];            // runs of so many pieces (kBins: that many or more), then where they go
   long long total = 0;
   for (int b = tid; b < a.B; b += 256) {
     const TreeLens t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
@@ -907,19 +901,52 @@ tree_prep_kernel(const TreePrepArgs a) {
   const long long up = (per + 255) / 256 * 256;
   const int run_len = (int)(up < 256 ? 256 : up > (1ll << 30) ? 1ll << 30 : up);      // (no sequence is longer than 2^30)
   int run0 = 0, item0 = 0, score0 = 0;
+  for (int k = tid; k <= kBins; k += 256) s_bin[k] = 0;
+  __syncthreads();
+  // runs of a sequence: their length, the pieces of one and of the last
+  auto cut = [&](const TreeLens& t, int& runs, int& len, int& pieces, int& pieces_last) {
+    runs = pieces = pieces_last = 0;
+    len = 256;
+    if (t.nodes == 0) return;                 // a sequence without nodes has only padding: zero rows
+    runs = (t.n + run_len - 1) / run_len;
+    len = ((t.n + runs - 1) / runs + 255) / 256 * 256;
+    runs = (t.n + len - 1) / len;
+    pieces = (len + kPiece - 1) / kPiece;
+    pieces_last = (t.n - (runs - 1) * len + kPiece - 1) / kPiece;
+  };
+  for (int b = tid; b < a.B; b += 256) {
+    int runs, len, pieces, last;
+    cut(tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len), runs, len, pieces, last);
+    if (runs > 1) atomicAdd(&s_bin[min(pieces, kBins)], runs - 1);
+    if (runs > 0) atomicAdd(&s_bin[min(last, kBins)], 1);
+  }
+  __syncthreads();
+  if (warp == 0) {                            // most pieces first: lane l adds up eight bins from the top
+    int v[8], sum = 0;
+    for (int e = 0; e < 8; ++e) {
+      v[e] = sum;
+      sum += s_bin[kBins - 8 * lane - e];
+    }
+    int before = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += y;
+    }
+    before -= sum;
+    __syncwarp();
+    for (int e = 0; e < 8; ++e) s_bin[kBins - 8 * lane - e] = before + v[e];
+  }
+  __syncthreads();
   for (int b0 = 0; b0 < a.B; b0 += 256) {
     const int b = b0 + tid;
     TreeLens t{0, 0, false};
-    int runs = 0, len = 256, items = 0, scores = 0;
-    if (b < a.B) t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
-    if (t.nodes > 0) {                        // a sequence without nodes has only padding: zero rows
-      runs = (t.n + run_len - 1) / run_len;
-      len = ((t.n + runs - 1) / runs + 255) / 256 * 256;
-      runs = (t.n + len - 1) / len;
-      const int last = t.n - (runs - 1) * len;
-      items = (runs - 1) * ((len + kPiece - 1) / kPiece) + (last + kPiece - 1) / kPiece;
-      scores = (t.n + 255) / 256;
+    int runs = 0, len = 256, pieces = 0, last = 0;
+    if (b < a.B) {
+      t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
+      cut(t, runs, len, pieces, last);
     }
+    const int items = runs > 0 ? (runs - 1) * pieces + last : 0, scores = runs > 0 ? (t.n + 255) / 256 : 0;
     int v[3] = {runs, items, scores}, x[3];
 #pragma unroll
     for (int e = 0; e < 3; ++e) {
@@ -942,9 +969,10 @@ tree_prep_kernel(const TreePrepArgs a) {
     if (b < a.B) {
       a.seq_first[b] = at;
       for (int k = 0; k < runs; ++k) {
-        const int tok = k * len, l = min(len, t.n - tok);
-        a.runs[2 * (at + k)] = make_int4(b, tok, l, (l + kPiece - 1) / kPiece);
-        a.runs[2 * (at + k) + 1] = make_int4(t.n, t.nodes, 0, 0);
+        const int tok = k * len, l = min(len, t.n - tok), np = k < runs - 1 ? pieces : last;
+        const int to = atomicAdd(&s_bin[min(np, kBins)], 1);      // (the order among equals is nobody's concern)
+        a.runs[2 * to] = make_int4(b, tok, l, np);
+        a.runs[2 * to + 1] = make_int4(t.n, t.nodes, at + k, 0);
       }
     }
     __syncthreads();
@@ -965,12 +993,12 @@ tree_prep_kernel(const TreePrepArgs a) {
 // ------------------------------------------------------------------ runs joined, W_uv
 // out[b,i,h,:] = (sum over runs 2^(m_run - M) acc_run / L) . W_uv,h: block = (head, 128 rows (b, i), a share of the latent
 // axis).  Per 64 latents the block joins the runs' fp32 rows (16 threads on 256 bytes of a row) into a bf16 head plus a
-// bf16 remainder, written as the A tile of two products with W_uv's [64 x d_h] block, which the copy engine brings three
-// steps ahead.  Blocks that share a tile's depth are a cluster; each adds its share of the columns over the others' sums in
+// bf16 remainder, written as the A tile of two products with W_uv's [64 x d_h] block, which the copy engine brings a
+// step ahead.  Blocks that share a tile's depth are a cluster; each adds its share of the columns over the others' sums in
 // block order through distributed shared memory.
-// Bound: the partial results, read once.
+// Bound: the partial results, read once: two blocks per SM, for bytes in flight.
 constexpr int kUpThreads = 256;
-constexpr int kUpW = 4;                   // W_uv blocks in flight
+constexpr int kUpW = 2;                   // W_uv blocks: in use and on its way
 constexpr int kUpHeld = 8;                // runs whose weights a row keeps
 
 struct UpArgs {
@@ -992,7 +1020,7 @@ struct UpSmem {
 };
 
 template <int KS, int G>
-__global__ void __launch_bounds__(kUpThreads, 1)
+__global__ void __launch_bounds__(kUpThreads, 2)
 tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -1032,8 +1060,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     mbar_expect_tx(fb, (uint32_t)wb);
     for (int j = 0; j < n_w; ++j) tma_load_2d(dst + j * 8192, &map_w, h * a.d_h + j * 64, c * 64, fb);
   };
-  if (tid == 0)
-    for (int c = c0; c < c1 && c < c0 + 2; ++c) load_w(c);
+  if (tid == 0 && c0 < c1) load_w(c0);
   ekv_pdl_wait();
   ekv_pdl_trigger();
 
@@ -1089,8 +1116,10 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   const uint32_t idesc = make_idesc(kRows, 16, 0, 1) + ((uint32_t)((a.d_h >> 3) - 2) << 17);
   constexpr uint32_t hi_sw = desc_hi(1024, 2);
   bool ok = true;
-  // one chunk: its first run's rows are in x, those of chunk c + 2 are requested
-  auto step = [&](int c, float4* x) {
+  float4 x[8];
+  fetch(c0, 0, x);
+#pragma unroll 1
+  for (int c = c0; c < c1 && ok; ++c) {
     const int st = (c - c0) & 1;
     float4 acc[8];
 #pragma unroll
@@ -1099,10 +1128,9 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
       // (a weight of zero keeps out what a row without a sum holds)
       acc[p] = w != 0.f ? make_float4(x[p].x * w, x[p].y * w, x[p].z * w, x[p].w * w) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    fetch(c + 2, 0, x);                    // in flight while this chunk is laid out and multiplied
+#pragma unroll 1
     for (int k0 = G; k0 < most; k0 += G) {
-      float4 y[8];
-      fetch(c, k0, y);
+      fetch(c, k0, x);
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
         const int row = row_t + 16 * (p / G), k = k0 + p % G;
@@ -1116,14 +1144,14 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
           }
         }
         if (w != 0.f) {
-          acc[p].x = fmaf(y[p].x, w, acc[p].x); acc[p].y = fmaf(y[p].y, w, acc[p].y);
-          acc[p].z = fmaf(y[p].z, w, acc[p].z); acc[p].w = fmaf(y[p].w, w, acc[p].w);
+          acc[p].x = fmaf(x[p].x, w, acc[p].x); acc[p].y = fmaf(x[p].y, w, acc[p].y);
+          acc[p].z = fmaf(x[p].z, w, acc[p].z); acc[p].w = fmaf(x[p].w, w, acc[p].w);
         }
       }
     }
+    fetch(c + 1, 0, x);                    // in flight while this chunk is laid out and multiplied
     // the products of chunk c - 2 have read the stage
     if (c - c0 >= 2) ok = mbar_wait(smem_u32(&bars->done[st]), (uint32_t)(((c - c0) >> 1) - 1) & 1, s_abort, 1);
-    if (tid == 0 && ok && c + 2 < c1) load_w(c + 2);
     unsigned char* const hi = base + st * 2 * kRows * 128;
 #pragma unroll
     for (int q = 0; q < 8 / G; ++q) {
@@ -1141,10 +1169,10 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     fence_proxy_async();
     ok = __syncthreads_and(ok) != 0;
     if (warp == 0 && ok) {
-      ok = warp_wait(smem_u32(&bars->w_full[(c - c0) % kUpW]), (uint32_t)((c - c0) / kUpW) & 1, s_abort, 2);
+      ok = warp_wait(smem_u32(&bars->w_full[st]), (uint32_t)((c - c0) >> 1) & 1, s_abort, 2);
       tc_fence_after();
       if (ok && elect_one()) {
-        const uint32_t la = desc_lo(smem_u32(hi), 16), lb = desc_lo(smem_u32(s_w) + (uint32_t)((c - c0) % kUpW) * wb, 8192);
+        const uint32_t la = desc_lo(smem_u32(hi), 16), lb = desc_lo(smem_u32(s_w) + (uint32_t)st * wb, 8192);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           tc_mma_w(tmem, la + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, c != c0 || k != 0);
@@ -1153,17 +1181,13 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
         tc_commit(smem_u32(&bars->done[st]));
       }
       __syncwarp();
+      // the next W_uv block, where the products of chunk c - 1 read theirs
+      if (ok && c + 1 < c1) {
+        if (c > c0) ok = warp_wait(smem_u32(&bars->done[st ^ 1]), (uint32_t)((c - 1 - c0) >> 1) & 1, s_abort, 5);
+        if (ok && lane == 0) load_w(c + 1);
+        __syncwarp();
+      }
     }
-  };
-  float4 x0[8], x1[8];
-  fetch(c0, 0, x0);
-  fetch(c0 + 1, 0, x1);
-#pragma unroll 1
-  for (int c = c0; c < c1; c += 2) {
-    step(c, x0);
-    if (!ok || c + 1 >= c1) break;
-    step(c + 1, x1);
-    if (!ok) break;
   }
   // the last products of both stages
   const int mine = c1 - c0;
@@ -1462,7 +1486,7 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   // shares of the depth while there are SMs for them, at least two steps each
   const long long tiles = L->n_h * (((long long)c.B * c.m + kRows - 1) / kRows);
   const int chunks = (L->vw + 63) / 64;
-  const int ks = tiles * 2 > L->sm_count || chunks < 4 ? 1 : tiles * 4 > L->sm_count || chunks < 8 ? 2 : 4;
+  const int ks = tiles > L->sm_count || chunks < 4 ? 1 : tiles * 2 > L->sm_count || chunks < 8 ? 2 : 4;
   auto launch_up = [&](auto kern) -> int {
     const size_t sm = UpSmem::total(L->d_h);
     EKV_CUDA_OK(ekv_allow_smem(kern, sm));
