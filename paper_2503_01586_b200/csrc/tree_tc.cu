@@ -50,7 +50,7 @@ constexpr int kMostAhead = kSlots - 8;  // D at most
 constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 loads cache rows, 3 clears drafted rows, 4-11 epilogue, 12 claims units
 constexpr int kEpiThreads = 128;         // a group of four epilogue warps
 constexpr int kQueue = 4;               // two units with the epilogue groups, two ahead (more would be late for those that wait for them)
-constexpr int kLead = 6;                // steps before a unit's last load at which the next unit is claimed
+constexpr int kLead = 16;                // steps before a unit's last load at which the next unit is claimed
 constexpr int kMaxStages = 6;
 constexpr int kABytes = kRows * 128;
 constexpr int kOutBytes = 4096;         // rows on their way out, per epilogue warp
@@ -71,7 +71,7 @@ struct TreeTcArgs {
   float2* pref;               // [slot][CG][128]: the same of the piece
   float2* cstate;             // [run][rb][ct][CG][128]: of the run so far
   int *s_cnt, *ready, *v_done, *chain;
-  float* part_acc;            // [run][rb][CG][128][vw]
+  float* part_acc;            // [run][rb][CG][vw / 64][128][64]
   float2* part_ml;            // [run][rb][CG][128]
   const int* hdr;             // [0] claim counter, [1] runs, [2] pieces (row blocks included), [3] D
   const int4* runs;           // [run][2], by pieces: (b, first token, tokens, pieces), (n, nodes, run, .)
@@ -223,6 +223,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   ekv_pdl_wait();
   ekv_pdl_trigger();
 
+  const int n_blk = (a.vw + 63) >> 6;                         // 64-column blocks of the partial result
   const int nkl = (a.kw + 63) >> 6, nkc = nkl + a.n_rc;       // steps of a score unit: latents, then rope columns
   // a published unit: what every role waits for, reads and gives back
   unsigned q_pos = 0;
@@ -743,7 +744,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (k_run > 0 && !group([&]() { return poll_global(a.chain + ci, k_run * CG, s_abort, 15); })) break;
         const float2 mine = __ldcg(a.pref + half * kRows + r);
         float2* const state = a.cstate + (ci * CG + rank) * kRows + r;
-        const long long tile_row = (((long long)run * a.n_rb + rb) * CG + rank) * kRows;      // of the block's rows in the partial result
+        const long long tile = ((long long)run * a.n_rb + rb) * CG + rank;      // the block's rows in the partial result
         float2 now = mine;
         float f_old = 1.f, f_new = 1.f;
         if (k_run > 0) {
@@ -760,14 +761,15 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const bool none = mine.y == 0.f;
         const bool scaled = __any_sync(0xffffffffu, f_old != 1.f);
         *state = now;
-        if (idx == 0) a.part_ml[tile_row + r] = now;
+        if (idx == 0) a.part_ml[tile * kRows + r] = now;
         auto chunk = [&](int cc, float* x) {              // 32 columns
           const int col = idx * kTile + cc * 32;
           if (col >= a.vw) return;                        // (the same for the whole warp)
+          const long long row0 = (tile * n_blk + (col >> 6)) * kRows;
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = spoiled ? __uint_as_float(0x7fffffffu) : none ? 0.f : x[e] * f_new;
           if (scaled) {                                   // references moved: what is there is scaled by its reader
-            const float* const o = a.part_acc + (tile_row + r) * a.vw + col;
+            const float* const o = a.part_acc + (row0 + r) * 64 + (col & 63);
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
               if (col + e < a.vw) {
@@ -788,8 +790,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             __syncwarp();
             if (lane == 0) {
               const uint32_t from = out_box + box * (kOutBytes / 2);
-              if (k_run == 0 || scaled) tma_store_2d(&map_o, col + box * 16, (int)(tile_row + quarter * 32), from);
-              else tma_add_2d(&map_o, col + box * 16, (int)(tile_row + quarter * 32), from);
+              if (k_run == 0 || scaled) tma_store_2d(&map_o, (col & 63) + box * 16, (int)row0 + quarter * 32, from);
+              else tma_add_2d(&map_o, (col & 63) + box * 16, (int)row0 + quarter * 32, from);
               bulk_commit_group();
             }
           }
@@ -991,14 +993,17 @@ tree_prep_kernel(const TreePrepArgs a) {
 }
 
 // ------------------------------------------------------------------ runs joined, W_uv
-// out[b,i,h,:] = (sum over runs 2^(m_run - M) acc_run / L) . W_uv,h: block = (head, 128 rows (b, i), a share of the latent
-// axis).  Per 64 latents the block joins the runs' fp32 rows (16 threads on 256 bytes of a row) into a bf16 head plus a
-// bf16 remainder, written as the A tile of two products with W_uv's [64 x d_h] block, which the copy engine brings a
-// step ahead.  Blocks that share a tile's depth are a cluster; each adds its share of the columns over the others' sums in
-// block order through distributed shared memory.
-// Bound: the partial results, read once: two blocks per SM, for bytes in flight.
-constexpr int kUpThreads = 256;
-constexpr int kUpW = 2;                   // W_uv blocks: in use and on its way
+// out[b,i,h,:] = (sum over runs 2^(m_run - M) acc_run / L) . W_uv,h: block = (head, as many whole sequences as 128 rows
+// (b, i) hold, a share of the latent axis).  The partial results lie in blocks of 64 latents, in which the m rows of a head
+// are one piece: bulk copies bring (64 latents, one run) of all rows into a ring, eight warps add them up with the runs'
+// weights and write a bf16 head plus a bf16 remainder as the A tile of two products with W_uv's [64 x d_h] block.  Blocks
+// that share a tile's depth are a cluster; each adds its share of the columns over the others' sums in block order through
+// distributed shared memory.
+// Bound: the partial results, read once; the ring keeps up to 96 KB of them in flight (32 KB, in registers, took 3 times
+// as long).
+constexpr int kUpThreads = 320;           // warps 0-7 join and lay out, 8 partial results, 9 products and W_uv
+constexpr int kUpSlots = 16;              // of the ring, at most
+constexpr int kUpRing = 96 * 1024;
 constexpr int kUpHeld = 8;                // runs whose weights a row keeps
 
 struct UpArgs {
@@ -1006,27 +1011,30 @@ struct UpArgs {
   const float2* part_ml;
   const int32_t* seq_first;
   bf16* out;
-  int B, m, n_h, d_h, hb, n_half, vw;
+  int B, m, n_h, d_h, hb, n_half, vw, spt, n_w, n_slots, slot_bytes;
   int32_t* status;
 };
-struct __align__(8) UpBars {
-  uint64_t w_full[kUpW], done[2];
+struct __align__(16) UpBars {
+  uint64_t full[kUpSlots], empty[kUpSlots], a_full[2], done[2], w_full[3];
 };
 struct UpSmem {
-  __host__ __device__ static constexpr int a_bytes() { return 2 * 2 * kRows * 128; }                 // 2 stages of head and remainder
+  static constexpr int a_bytes = 2 * 2 * kRows * 128;                 // 2 stages of head and remainder
+  static constexpr int misc = sizeof(UpBars) + 16 + kRows * (kUpHeld * 4 + 16);
   __host__ __device__ static constexpr int w_block(int d_h) { return (d_h + 63) / 64 * 8192; }
-  __host__ __device__ static constexpr int misc() { return sizeof(UpBars) + 16 + kRows * (kUpHeld * 4 + 16); }
-  __host__ __device__ static constexpr int total(int d_h) { return a_bytes() + kUpW * w_block(d_h) + misc() + 1024; }
+  __host__ __device__ static constexpr int n_w(int d_h) { return d_h <= 128 ? 3 : 2; }
+  __host__ __device__ static constexpr int ring(int d_h) { return d_h <= 128 ? kUpRing : kUpRing - 32 * 1024; }
+  __host__ __device__ static constexpr int total(int d_h) { return a_bytes + n_w(d_h) * w_block(d_h) + ring(d_h) + misc + 1024; }
 };
 
-template <int KS, int G>
-__global__ void __launch_bounds__(kUpThreads, 2)
+template <int KS>
+__global__ void __launch_bounds__(kUpThreads, 1)
 tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int wb = UpSmem::w_block(a.d_h);
-  unsigned char* const s_w = base + UpSmem::a_bytes();
-  UpBars* const bars = (UpBars*)(s_w + kUpW * wb);
+  unsigned char* const s_w = base + UpSmem::a_bytes;
+  unsigned char* const s_ring = s_w + a.n_w * wb;
+  UpBars* const bars = (UpBars*)(s_ring + UpSmem::ring(a.d_h));
   uint32_t* const s_tmem = (uint32_t*)(bars + 1);
   volatile int* const s_abort = (volatile int*)(s_tmem + 1);
   float* const s_wt = (float*)(s_tmem + 4);              // [128][kUpHeld] normalised weights of a row's runs
@@ -1034,19 +1042,25 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   int2* const s_run = (int2*)(s_ml + kRows);             // [128] first run, runs
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, z = KS > 1 ? (int)cluster_ctarank() : 0;
-  const long long n_rows = (long long)a.B * a.m, r0 = (long long)blockIdx.x * kRows;
+  const int b0 = blockIdx.x * a.spt, n_seq = min(a.spt, a.B - b0), n_rows = n_seq * a.m;       // this block's sequences and rows
   const int chunks = (a.vw + 63) >> 6, c0 = chunks * z / KS, c1 = chunks * (z + 1) / KS;
-  const int n_w = (a.d_h + 63) >> 6;
   const uint32_t cols = a.d_h <= 32 ? 32 : a.d_h <= 64 ? 64 : a.d_h <= 128 ? 128 : 256;
 
   if (tid == 0) {
-    for (int i = 0; i < kUpW; ++i) mbar_init(smem_u32(&bars->w_full[i]), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->done[i]), 1);
+    for (int i = 0; i < kUpSlots; ++i) {
+      mbar_init(smem_u32(&bars->full[i]), 1);
+      mbar_init(smem_u32(&bars->empty[i]), 8);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars->a_full[i]), 8);
+      mbar_init(smem_u32(&bars->done[i]), 1);
+    }
+    for (int i = 0; i < 3; ++i) mbar_init(smem_u32(&bars->w_full[i]), 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
-  if (warp == 1) {
+  if (warp == 9) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -1054,25 +1068,26 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
-  // W_uv's block of chunk c (the layer's own copy: no kernel writes it)
-  auto load_w = [&](int c) {
-    const uint32_t fb = smem_u32(&bars->w_full[(c - c0) % kUpW]), dst = smem_u32(s_w) + (uint32_t)((c - c0) % kUpW) * wb;
+  // W_uv's block of this block's q-th chunk (the layer's own copy: no kernel writes it)
+  auto load_w = [&](int q) {
+    const uint32_t fb = smem_u32(&bars->w_full[q % a.n_w]), dst = smem_u32(s_w) + (uint32_t)(q % a.n_w) * wb;
     mbar_expect_tx(fb, (uint32_t)wb);
-    for (int j = 0; j < n_w; ++j) tma_load_2d(dst + j * 8192, &map_w, h * a.d_h + j * 64, c * 64, fb);
+    for (int j = 0; j < wb / 8192; ++j) tma_load_2d(dst + j * 8192, &map_w, h * a.d_h + j * 64, (c0 + q) * 64, fb);
   };
-  if (tid == 0 && c0 < c1) load_w(c0);
+  const int mine = c1 - c0;
+  if (tid == 288)
+    for (int q = 0; q < mine && q < a.n_w - 1; ++q) load_w(q);
   ekv_pdl_wait();
   ekv_pdl_trigger();
 
   // ---- a row's runs, its largest reference and its sum
-  const int half = h / a.hb, hr = (h - half * a.hb) * a.m;
+  const int half = h / a.hb, hr = (h - half * a.hb) * a.m;      // the head's rows in a tile of the partial results
   if (tid < kRows) {
-    const long long R = r0 + tid;
     int2 run = make_int2(0, 0);
     float M = -1e30f, L = 0.f;
     const float2* ml = a.part_ml;
-    if (R < n_rows) {
-      const int b = (int)(R / a.m), i = (int)(R - (long long)b * a.m);
+    if (tid < n_rows) {
+      const int b = b0 + tid / a.m, i = tid % a.m;
       run.x = __ldcg(a.seq_first + b);
       run.y = __ldcg(a.seq_first + b + 1) - run.x;
       ml += ((long long)run.x * a.n_half + half) * kRows + hr + i;
@@ -1088,125 +1103,131 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     s_run[tid] = run;
   }
   __syncthreads();
-
-  // 4 of a chunk's columns of the rows row_t + 16 q; G: calls of few rows have G runs of a row fetched at once
-  constexpr int kQ = 8 / G;
-  const int col4 = tid & 15, row_t = tid >> 4;
-  const float* src[kQ];
-  int n_run[kQ], most = 0;
-#pragma unroll
-  for (int q = 0; q < kQ; ++q) {
-    const int row = row_t + 16 * q;
-    const long long R = r0 + row;
-    const int2 run = s_run[row];
-    const int i = (int)(R % a.m);
-    n_run[q] = R < n_rows ? run.y : 0;
-    src[q] = a.part_acc + (((long long)run.x * a.n_half + half) * kRows + hr + i) * a.vw + col4 * 4;
-    most = max(most, n_run[q]);
-  }
-  const long long run_pitch = (long long)a.n_half * kRows * a.vw;
-  auto fetch = [&](int c, int k0, float4* x) {           // runs k0 .. k0 + G - 1 of chunk c
-    const bool in = c < c1 && c * 64 + col4 * 4 < a.vw;
-#pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const int q = p / G, k = k0 + p % G;
-      x[p] = in && k < n_run[q] ? __ldcg((const float4*)(src[q] + k * run_pitch + c * 64)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-  };
-  const uint32_t idesc = make_idesc(kRows, 16, 0, 1) + ((uint32_t)((a.d_h >> 3) - 2) << 17);
-  constexpr uint32_t hi_sw = desc_hi(1024, 2);
+  int most = 0;
+  for (int k = lane; k < n_rows; k += 32) most = max(most, s_run[k].y);
+  most = __reduce_max_sync(0xffffffffu, most);
+  const int steps = max(most, 1);                        // units of a chunk (no runs at all: a tile of zeros)
   bool ok = true;
-  float4 x[8];
-  fetch(c0, 0, x);
-#pragma unroll 1
-  for (int c = c0; c < c1 && ok; ++c) {
-    const int st = (c - c0) & 1;
-    float4 acc[8];
-#pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const float w = s_wt[(row_t + 16 * (p / G)) * kUpHeld + p % G];
-      // (a weight of zero keeps out what a row without a sum holds)
-      acc[p] = w != 0.f ? make_float4(x[p].x * w, x[p].y * w, x[p].z * w, x[p].w * w) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll 1
-    for (int k0 = G; k0 < most; k0 += G) {
-      fetch(c, k0, x);
-#pragma unroll
-      for (int p = 0; p < 8; ++p) {
-        const int row = row_t + 16 * (p / G), k = k0 + p % G;
-        float w = 0.f;
-        if (k < n_run[p / G]) {
-          if (k < kUpHeld) {
-            w = s_wt[row * kUpHeld + k];
-          } else {
-            const long long R = r0 + row;
-            w = exp2f(__ldcg(a.part_ml + ((long long)(s_run[row].x + k) * a.n_half + half) * kRows + hr + (int)(R % a.m)).x - s_ml[row].x) * s_ml[row].y;
-          }
+
+  if (warp == 8) {
+    // ---- partial results: unit (chunk, k-th run of every sequence)
+    int u = 0;
+    for (int q = 0; q < mine && ok; ++q)
+      for (int k = 0; k < steps; ++k, ++u) {
+        const int slot = u % a.n_slots;
+        ok = warp_wait(smem_u32(&bars->empty[slot]), ((u / a.n_slots) & 1) ^ 1, s_abort, 1);
+        if (!ok) break;
+        int n = 0;
+        for (int e = 0; e < n_seq; e += 32) n += __popc(__ballot_sync(0xffffffffu, e + lane < n_seq && s_run[min(e + lane, n_seq - 1) * a.m].y > k));
+        const uint32_t fb = smem_u32(&bars->full[slot]), dst = smem_u32(s_ring) + (uint32_t)slot * a.slot_bytes;
+        if (lane == 0) mbar_expect_tx(fb, (uint32_t)(n * a.m * 256));
+        __syncwarp();
+        for (int e = lane; e < n_seq; e += 32) {
+          const int2 run = s_run[e * a.m];
+          if (run.y > k)
+            bulk_load(dst + e * a.m * 256, a.part_acc + ((((long long)run.x + k) * a.n_half + half) * chunks + c0 + q) * kRows * 64 + hr * 64, (uint32_t)a.m * 256, fb);
         }
-        if (w != 0.f) {
-          acc[p].x = fmaf(x[p].x, w, acc[p].x); acc[p].y = fmaf(x[p].y, w, acc[p].y);
-          acc[p].z = fmaf(x[p].z, w, acc[p].z); acc[p].w = fmaf(x[p].w, w, acc[p].w);
-        }
+        __syncwarp();
       }
-    }
-    fetch(c + 1, 0, x);                    // in flight while this chunk is laid out and multiplied
-    // the products of chunk c - 2 have read the stage
-    if (c - c0 >= 2) ok = mbar_wait(smem_u32(&bars->done[st]), (uint32_t)(((c - c0) >> 1) - 1) & 1, s_abort, 1);
-    unsigned char* const hi = base + st * 2 * kRows * 128;
-#pragma unroll
-    for (int q = 0; q < 8 / G; ++q) {
-      const int row = row_t + 16 * q;
-      float4 v = acc[q * G];
-#pragma unroll
-      for (int g = 1; g < G; ++g) { v.x += acc[q * G + g].x; v.y += acc[q * G + g].y; v.z += acc[q * G + g].z; v.w += acc[q * G + g].w; }
-      const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
-      const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
-      const bf162 l0 = __floats2bfloat162_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2bfloat162_rn(v.z - f1.x, v.w - f1.y);
-      const int at = row * 128 + (((col4 >> 1) ^ (row & 7)) << 4) + (col4 & 1) * 8;
-      *(uint2*)(hi + at) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
-      *(uint2*)(hi + kRows * 128 + at) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
-    }
-    fence_proxy_async();
-    ok = __syncthreads_and(ok) != 0;
-    if (warp == 0 && ok) {
-      ok = warp_wait(smem_u32(&bars->w_full[st]), (uint32_t)((c - c0) >> 1) & 1, s_abort, 2);
+  } else if (warp == 9) {
+    // ---- products
+    const uint32_t idesc = make_idesc(kRows, 16, 0, 1) + ((uint32_t)((a.d_h >> 3) - 2) << 17);
+    constexpr uint32_t hi_sw = desc_hi(1024, 2);
+    for (int q = 0; q < mine && ok; ++q) {
+      const int st = q & 1;
+      ok = warp_wait(smem_u32(&bars->a_full[st]), (q >> 1) & 1, s_abort, 2) &&
+           warp_wait(smem_u32(&bars->w_full[q % a.n_w]), (q / a.n_w) & 1, s_abort, 3);
+      if (!ok) break;
       tc_fence_after();
-      if (ok && elect_one()) {
-        const uint32_t la = desc_lo(smem_u32(hi), 16), lb = desc_lo(smem_u32(s_w) + (uint32_t)st * wb, 8192);
+      if (elect_one()) {
+        const uint32_t la = desc_lo(smem_u32(base) + st * 2 * kRows * 128, 16), lb = desc_lo(smem_u32(s_w) + (uint32_t)(q % a.n_w) * wb, 8192);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          tc_mma_w(tmem, la + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, c != c0 || k != 0);
+          tc_mma_w(tmem, la + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, q != 0 || k != 0);
           tc_mma_w(tmem, la + (kRows * 128 >> 4) + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, 1);
         }
         tc_commit(smem_u32(&bars->done[st]));
       }
       __syncwarp();
-      // the next W_uv block, where the products of chunk c - 1 read theirs
-      if (ok && c + 1 < c1) {
-        if (c > c0) ok = warp_wait(smem_u32(&bars->done[st ^ 1]), (uint32_t)((c - 1 - c0) >> 1) & 1, s_abort, 5);
-        if (ok && lane == 0) load_w(c + 1);
+      // the W_uv block after the next goes where the products before these read theirs
+      if (q + a.n_w - 1 < mine) {
+        if (q > 0) ok = warp_wait(smem_u32(&bars->done[st ^ 1]), ((q - 1) >> 1) & 1, s_abort, 4);
+        if (ok && lane == 0) load_w(q + a.n_w - 1);
         __syncwarp();
       }
     }
+  } else {
+    // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 16 p
+    const int col4 = tid & 15, row_t = tid >> 4;
+    int u = 0;
+    for (int q = 0; q < mine; ++q) {
+      const int st = q & 1;
+      const bool in = (c0 + q) * 64 + col4 * 4 < a.vw;
+      float4 acc[8];
+#pragma unroll
+      for (int p = 0; p < 8; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < steps; ++k, ++u) {
+        const int slot = u % a.n_slots;
+        ok = ok && mbar_wait(smem_u32(&bars->full[slot]), (u / a.n_slots) & 1, s_abort, 5);
+        if (ok) {
+          const unsigned char* const src = s_ring + (size_t)slot * a.slot_bytes + col4 * 16;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            const int row = row_t + 16 * p;
+            if (row >= n_rows) continue;
+            float w;
+            if (k < kUpHeld) {
+              w = s_wt[row * kUpHeld + k];
+            } else {
+              w = k < s_run[row].y ? exp2f(__ldcg(a.part_ml + ((long long)(s_run[row].x + k) * a.n_half + half) * kRows + hr + row % a.m).x - s_ml[row].x) * s_ml[row].y : 0.f;
+            }
+            if (w != 0.f && in) {          // (a weight of zero keeps out what a row without a sum holds)
+              const float4 x = *(const float4*)(src + row * 256);
+              acc[p].x = fmaf(x.x, w, acc[p].x); acc[p].y = fmaf(x.y, w, acc[p].y);
+              acc[p].z = fmaf(x.z, w, acc[p].z); acc[p].w = fmaf(x.w, w, acc[p].w);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->empty[slot]));
+      }
+      // the products of chunk q - 2 have read the stage
+      if (q >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[st]), ((q >> 1) - 1) & 1, s_abort, 6);
+      unsigned char* const hi = base + st * 2 * kRows * 128;
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        const int row = row_t + 16 * p;
+        if (row >= n_rows) continue;       // (rows of nobody hold anything)
+        const float4 v = acc[p];
+        const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
+        const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
+        const bf162 l0 = __floats2bfloat162_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2bfloat162_rn(v.z - f1.x, v.w - f1.y);
+        const int at = row * 128 + (((col4 >> 1) ^ (row & 7)) << 4) + (col4 & 1) * 8;
+        *(uint2*)(hi + at) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
+        *(uint2*)(hi + kRows * 128 + at) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->a_full[st]));
+    }
+    // the last products of both stages
+    if (mine >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[mine & 1]), ((mine - 2) >> 1) & 1, s_abort, 7);
+    if (mine >= 1) ok = ok && mbar_wait(smem_u32(&bars->done[(mine - 1) & 1]), ((mine - 1) >> 1) & 1, s_abort, 8);
   }
-  // the last products of both stages
-  const int mine = c1 - c0;
-  if (ok && mine >= 2) ok = mbar_wait(smem_u32(&bars->done[mine & 1]), (uint32_t)((mine - 2) >> 1) & 1, s_abort, 3);
-  if (ok && mine >= 1) ok = mbar_wait(smem_u32(&bars->done[(mine - 1) & 1]), (uint32_t)((mine - 1) >> 1) & 1, s_abort, 4);
+  __syncwarp();
   tc_fence_after();
   ok = __syncthreads_and(ok) != 0;
 
   const int quarter = warp & 3, part = warp >> 2;        // rows of a warp; two warps share its columns, 8 at a time
   const int row = quarter * 32 + lane;
-  const long long R = r0 + row;
-  bf16* const dst = a.out + (R * a.n_h + h) * a.d_h;
+  bf16* const dst = a.out + (((long long)b0 * a.m + row) * a.n_h + h) * a.d_h;
   const uint32_t tm = tmem + ((uint32_t)(quarter * 32) << 16);
   if (KS == 1) {
-    for (int c = part * 8; c < a.d_h && ok; c += 16) {
+    for (int c = part * 8; c < a.d_h && ok && warp < 8; c += 16) {
       float v[8];
       tc_ld8(tm + c, v);
       tc_wait_ld();
-      if (R < n_rows) {
+      if (row < n_rows) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) *(bf162*)(dst + c + 2 * e) = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
       }
@@ -1215,9 +1236,10 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   } else {
     // every block sends its sums of columns [q w, (q + 1) w) to block q
     const int w = a.d_h / KS;
-    float* const recv = (float*)base;                    // [source][column][row]
-    cluster_sync_all();                                  // all products are done: the stages are free in every block
-    for (int c = part * 8; c < a.d_h; c += 16) {
+    float* const recv = (float*)base;                    // [source][column][row], over stages and ring
+    static_assert(kRows * 256 * 4 <= UpSmem::a_bytes + kUpRing - 32 * 1024, "the sums of a tile fit");
+    cluster_sync_all();                                  // all bulk copies have landed and all products are done in every block
+    for (int c = part * 8; c < a.d_h && warp < 8; c += 16) {
       float v[8];
       tc_ld8(tm + c, v);
       tc_wait_ld();
@@ -1229,7 +1251,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     }
     __syncwarp();
     cluster_sync_all();
-    if (R < n_rows && ok) {
+    if (row < n_rows && ok && warp < 8) {
       for (int k = part * 2; k < w; k += 4) {
         float s0 = 0.f, s1 = 0.f;
 #pragma unroll
@@ -1245,7 +1267,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   __syncthreads();
   if (*s_abort) drain_after_abort();
   if (tid == 0 && *s_abort) ekv_record(a.status, ELITEKV_ERR_TIMEOUT, (int)blockIdx.x | (*s_abort << 16), (int)blockIdx.y);
-  if (warp == 1) {
+  if (warp == 9) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
   }
@@ -1297,7 +1319,7 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.qr = o;     o = align256(o + sizeof(bf16) * (size_t)B * s.n_rb * s.cg * s.n_rc * kRows * 64);
   const size_t tile_rows = c.max_runs * s.n_rb * s.cg * kRows;
   c.ml = o;     o = align256(o + sizeof(float2) * tile_rows);
-  c.acc = o;    o = align256(o + sizeof(float) * tile_rows * L->vw);
+  c.acc = o;    o = align256(o + sizeof(float) * tile_rows * ((L->vw + 63) / 64) * 64);
   c.total = o;
   return c;
 }
@@ -1356,7 +1378,7 @@ size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m) { return tree_car
 // rope rows whole 16 bytes.
 int ekv_tree_tc_supported(const elitekv_layer* L, int B, int m, const CacheView* cv) {
   const TreeShape s = tree_shape(L, m);
-  if (((unsigned long long)B + s.want) * s.n_rb * s.cg * kRows >= (1ull << 31) ||
+  if (((unsigned long long)B + s.want) * s.n_rb * s.cg * ((L->vw + 63) / 64) * kRows >= (1ull << 31) ||
       (unsigned long long)B * s.n_rb * s.cg * s.n_rc * kRows >= (1ull << 31) || L->n_h > 65535)
     return 0;
   if ((L->n_h * L->r) % 4 != 0) return 0;
@@ -1402,7 +1424,7 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.status = L->d_status;
   CUtensorMap m_q, m_k, m_v, m_p, m_qr, m_r, m_ps, m_o, m_w;
   a.v3 = a.box_v == 64 && L->vw % 64 == 0;
-  const unsigned long long tile_rows = (unsigned long long)w.max_runs * s.n_rb * s.cg * kRows;
+  const unsigned long long blk_rows = (unsigned long long)w.max_runs * s.n_rb * s.cg * ((L->vw + 63) / 64) * kRows;
   const unsigned long long rows = plane_rows(cv);
   int rc = make_map_queries(&m_q, c.q_abs, c.B, c.m, L->n_h, L->kw, s.hb);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_k, cache->latent, rows, L->kw, L->d_c, a.box_s);
@@ -1410,7 +1432,7 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
     rc = a.v3 ? make_map_chunks(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, 4 / s.cg)
               : make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
   if (rc == ELITEKV_OK) rc = make_map_box(&m_ps, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, 2);
-  if (rc == ELITEKV_OK) rc = make_map_box(&m_o, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a.part_acc, tile_rows, L->vw, 4);
+  if (rc == ELITEKV_OK) rc = make_map_box(&m_o, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a.part_acc, blk_rows, 64, 4);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_w, L->d_Wuv, L->vw, (unsigned long long)L->n_h * L->d_h, (unsigned long long)L->n_h * L->d_h, 64);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, kRows);
   // (a layer without rope has neither; the maps are not used)
@@ -1483,15 +1505,25 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   u.n_half = s.n_rb * s.cg;
   u.vw = L->vw;
   u.status = L->d_status;
-  // shares of the depth while there are SMs for them, at least two steps each
-  const long long tiles = L->n_h * (((long long)c.B * c.m + kRows - 1) / kRows);
+  u.spt = kRows / c.m;
+  u.n_w = UpSmem::n_w(L->d_h);
+  u.slot_bytes = (c.B < u.spt ? c.B : u.spt) * c.m * 256;
+  u.n_slots = UpSmem::ring(L->d_h) / u.slot_bytes < kUpSlots ? UpSmem::ring(L->d_h) / u.slot_bytes : kUpSlots;
+  // shares of the depth: a block takes a step per 64 latents and about four more to start and end
+  const long long groups = (c.B + u.spt - 1) / u.spt, tiles = L->n_h * groups;
   const int chunks = (L->vw + 63) / 64;
-  const int ks = tiles > L->sm_count || chunks < 4 ? 1 : tiles * 2 > L->sm_count || chunks < 8 ? 2 : 4;
+  int ks = 1;
+  long long best = 0;
+  for (int k = 1; k <= 4 && k <= chunks; k *= 2) {
+    if (L->d_h % (4 * k) != 0) break;
+    const long long t = (tiles * k + L->sm_count - 1) / L->sm_count * ((chunks + k - 1) / k + 4);
+    if (k == 1 || t < best) { best = t; ks = k; }
+  }
   auto launch_up = [&](auto kern) -> int {
     const size_t sm = UpSmem::total(L->d_h);
     EKV_CUDA_OK(ekv_allow_smem(kern, sm));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles / L->n_h), (unsigned)L->n_h, (unsigned)ks);
+    cfg.gridDim = dim3((unsigned)groups, (unsigned)L->n_h, (unsigned)ks);
     cfg.blockDim = dim3(kUpThreads);
     cfg.dynamicSmemBytes = sm;
     cfg.stream = st;
@@ -1508,8 +1540,5 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
     EKV_CUDA_OK(cudaGetLastError());
     return ELITEKV_OK;
   };
-  const long long up_rows = (long long)c.B * c.m;         // of the only row block, where there is one
-  if (up_rows <= 16) return ks == 4 ? launch_up(tree_up_kernel<4, 8>) : ks == 2 ? launch_up(tree_up_kernel<2, 8>) : launch_up(tree_up_kernel<1, 8>);
-  if (up_rows <= 64) return ks == 4 ? launch_up(tree_up_kernel<4, 2>) : ks == 2 ? launch_up(tree_up_kernel<2, 2>) : launch_up(tree_up_kernel<1, 2>);
-  return ks == 4 ? launch_up(tree_up_kernel<4, 1>) : ks == 2 ? launch_up(tree_up_kernel<2, 1>) : launch_up(tree_up_kernel<1, 1>);
+  return ks == 4 ? launch_up(tree_up_kernel<4>) : ks == 2 ? launch_up(tree_up_kernel<2>) : launch_up(tree_up_kernel<1>);
 }
