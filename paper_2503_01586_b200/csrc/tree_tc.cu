@@ -229,10 +229,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   unsigned q_pos = 0;
   auto q_slot = [&]() { return q_pos % kQueue; };
   auto q_parity = [&]() { return (q_pos / kQueue) & 1u; };
-  auto release_unit = [&]() {                        // one lane of a warp
-    const uint32_t bar = smem_u32(&bars->q_empty[q_slot()]);
-    if (CG == 2) mbar_arrive_cluster(map_to_cta(bar, 0)); else mbar_arrive(bar);
+  // Arrival on a barrier of the first block that only says "read": what it stands for (words of shared memory, tensor memory
+  // that tcgen05.wait::ld has waited for) is in registers.  (With release semantics over the cluster it held the warp
+  // that issues the products for 2500 clocks a unit.)
+  auto arrive_read = [&](uint32_t bar) {             // one lane of a warp
+    if (rank == 0) mbar_arrive(bar); else mbar_arrive_cluster_relaxed(map_to_cta(bar, 0));
   };
+  auto release_unit = [&]() { arrive_read(smem_u32(&bars->q_empty[q_slot()])); };
 
   if (warp == 0) {
     // ============================================================== queries, P (and the bytes that a step expects)
@@ -611,10 +614,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       auto acc_done = [&]() {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          const uint32_t bar = smem_u32(&bars->acc_empty[group_id]);
-          if (CG == 2) mbar_arrive_cluster(map_to_cta(bar, 0)); else mbar_arrive(bar);
-        }
+        if (lane == 0) arrive_read(smem_u32(&bars->acc_empty[group_id]));
       };
       if (type == kScore) {
         const int t0 = tok0 + idx * kTile;
@@ -1001,7 +1001,8 @@ tree_prep_kernel(const TreePrepArgs a) {
 // distributed shared memory.
 // Bound: the partial results, read once; the ring keeps up to 96 KB of them in flight (32 KB, in registers, took 3 times
 // as long).
-constexpr int kUpThreads = 320;           // warps 0-7 join and lay out, 8 partial results, 9 products and W_uv
+constexpr int kUpWarps = 16;              // that join and lay out; one more for partial results, one for products and W_uv
+constexpr int kUpThreads = 32 * (kUpWarps + 2);
 constexpr int kUpSlots = 16;              // of the ring, at most
 constexpr int kUpRing = 96 * 1024;
 constexpr int kUpHeld = 8;                // runs whose weights a row keeps
@@ -1011,7 +1012,7 @@ struct UpArgs {
   const float2* part_ml;
   const int32_t* seq_first;
   bf16* out;
-  int B, m, n_h, d_h, hb, n_half, vw, spt, n_w, n_slots, slot_bytes;
+  int B, m, n_h, d_h, hb, n_half, vw, spt, n_w, n_slots, slot_bytes, group;
   int32_t* status;
 };
 struct __align__(16) UpBars {
@@ -1049,10 +1050,10 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   if (tid == 0) {
     for (int i = 0; i < kUpSlots; ++i) {
       mbar_init(smem_u32(&bars->full[i]), 1);
-      mbar_init(smem_u32(&bars->empty[i]), 8);
+      mbar_init(smem_u32(&bars->empty[i]), kUpWarps);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&bars->a_full[i]), 8);
+      mbar_init(smem_u32(&bars->a_full[i]), kUpWarps);
       mbar_init(smem_u32(&bars->done[i]), 1);
     }
     for (int i = 0; i < 3; ++i) mbar_init(smem_u32(&bars->w_full[i]), 1);
@@ -1060,7 +1061,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
-  if (warp == 9) {
+  if (warp == kUpWarps + 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -1075,7 +1076,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     for (int j = 0; j < wb / 8192; ++j) tma_load_2d(dst + j * 8192, &map_w, h * a.d_h + j * 64, (c0 + q) * 64, fb);
   };
   const int mine = c1 - c0;
-  if (tid == 288)
+  if (tid == 32 * (kUpWarps + 1))
     for (int q = 0; q < mine && q < a.n_w - 1; ++q) load_w(q);
   ekv_pdl_wait();
   ekv_pdl_trigger();
@@ -1085,20 +1086,32 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   if (tid < kRows) {
     int2 run = make_int2(0, 0);
     float M = -1e30f, L = 0.f;
+    float2 held[kUpHeld];
+#pragma unroll
+    for (int k = 0; k < kUpHeld; ++k) held[k] = make_float2(-1e30f, 0.f);
     const float2* ml = a.part_ml;
+    const long long pitch = (long long)a.n_half * kRows;
     if (tid < n_rows) {
       const int b = b0 + tid / a.m, i = tid % a.m;
       run.x = __ldcg(a.seq_first + b);
       run.y = __ldcg(a.seq_first + b + 1) - run.x;
-      ml += ((long long)run.x * a.n_half + half) * kRows + hr + i;
-      for (int k = 0; k < run.y; ++k) M = fmaxf(M, __ldcg(ml + (long long)k * a.n_half * kRows).x);
-      for (int k = 0; k < run.y; ++k) {
-        const float2 x = __ldcg(ml + (long long)k * a.n_half * kRows);
+      ml += run.x * pitch + half * kRows + hr + i;
+#pragma unroll
+      for (int k = 0; k < kUpHeld; ++k)
+        if (k < run.y) held[k] = __ldcg(ml + k * pitch);
+#pragma unroll
+      for (int k = 0; k < kUpHeld; ++k) M = fmaxf(M, held[k].x);
+      for (int k = kUpHeld; k < run.y; ++k) M = fmaxf(M, __ldcg(ml + k * pitch).x);
+#pragma unroll
+      for (int k = 0; k < kUpHeld; ++k) L = fmaf(held[k].y, exp2f(held[k].x - M), L);
+      for (int k = kUpHeld; k < run.y; ++k) {
+        const float2 x = __ldcg(ml + k * pitch);
         L = fmaf(x.y, exp2f(x.x - M), L);
       }
     }
     const float inv = L != 0.f ? 1.f / L : 0.f;          // (nothing seen: a zero row)
-    for (int k = 0; k < kUpHeld; ++k) s_wt[tid * kUpHeld + k] = k < run.y ? exp2f(__ldcg(ml + (long long)k * a.n_half * kRows).x - M) * inv : 0.f;
+#pragma unroll
+    for (int k = 0; k < kUpHeld; ++k) s_wt[tid * kUpHeld + k] = k < run.y ? exp2f(held[k].x - M) * inv : 0.f;
     s_ml[tid] = make_float2(M, inv);
     s_run[tid] = run;
   }
@@ -1106,30 +1119,51 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   int most = 0;
   for (int k = lane; k < n_rows; k += 32) most = max(most, s_run[k].y);
   most = __reduce_max_sync(0xffffffffu, most);
-  const int steps = max(most, 1);                        // units of a chunk (no runs at all: a tile of zeros)
+  const int steps = max((most + a.group - 1) / a.group, 1);     // units of a chunk (no runs at all: a tile of zeros)
   bool ok = true;
+  // normalised weight of a row's k-th run (0: there is none)
+  auto weight = [&](int row, int k) -> float {
+    if (k < kUpHeld) return s_wt[row * kUpHeld + k];
+    if (k >= s_run[row].y) return 0.f;
+    return exp2f(__ldcg(a.part_ml + ((long long)(s_run[row].x + k) * a.n_half + half) * kRows + hr + row % a.m).x - s_ml[row].x) * s_ml[row].y;
+  };
 
-  if (warp == 8) {
-    // ---- partial results: unit (chunk, k-th run of every sequence)
-    int u = 0;
+  if (warp == kUpWarps) {
+    // ---- partial results: unit (chunk, `group` runs of every sequence).  A lane copies up to four (run, sequence) pairs.
+    const float* src[4];
+    int left[4], to[4];                    // runs of the sequence from this one on; place in the unit
+    const int pairs = a.group * n_seq;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int x = lane + 32 * t, g = x / n_seq, e = x - g * n_seq;
+      const int2 run = x < pairs ? s_run[e * a.m] : make_int2(0, 0);
+      left[t] = x < pairs ? run.y - g : 0;
+      to[t] = (g * n_rows + e * a.m) * 256;
+      src[t] = a.part_acc + (((long long)run.x + g) * a.n_half + half) * chunks * kRows * 64 + hr * 64;
+    }
+    const long long run_pitch = (long long)a.n_half * chunks * kRows * 64;
+    const uint32_t bytes = (uint32_t)a.m * 256;
+    int slot = 0;
+    uint32_t turn = 1;
     for (int q = 0; q < mine && ok; ++q)
-      for (int k = 0; k < steps; ++k, ++u) {
-        const int slot = u % a.n_slots;
-        ok = warp_wait(smem_u32(&bars->empty[slot]), ((u / a.n_slots) & 1) ^ 1, s_abort, 1);
+      for (int k = 0; k < steps; ++k) {
+        ok = warp_wait(smem_u32(&bars->empty[slot]), turn, s_abort, 1);
         if (!ok) break;
+        const int k0 = k * a.group;
         int n = 0;
-        for (int e = 0; e < n_seq; e += 32) n += __popc(__ballot_sync(0xffffffffu, e + lane < n_seq && s_run[min(e + lane, n_seq - 1) * a.m].y > k));
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (32 * t < pairs) n += __popc(__ballot_sync(0xffffffffu, left[t] > k0));
         const uint32_t fb = smem_u32(&bars->full[slot]), dst = smem_u32(s_ring) + (uint32_t)slot * a.slot_bytes;
-        if (lane == 0) mbar_expect_tx(fb, (uint32_t)(n * a.m * 256));
+        if (lane == 0) mbar_expect_tx(fb, (uint32_t)n * bytes);
         __syncwarp();
-        for (int e = lane; e < n_seq; e += 32) {
-          const int2 run = s_run[e * a.m];
-          if (run.y > k)
-            bulk_load(dst + e * a.m * 256, a.part_acc + ((((long long)run.x + k) * a.n_half + half) * chunks + c0 + q) * kRows * 64 + hr * 64, (uint32_t)a.m * 256, fb);
-        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (left[t] > k0) bulk_load(dst + to[t], src[t] + k0 * run_pitch + (long long)(c0 + q) * kRows * 64, bytes, fb);
         __syncwarp();
+        if (++slot == a.n_slots) { slot = 0; turn ^= 1; }
       }
-  } else if (warp == 9) {
+  } else if (warp == kUpWarps + 1) {
     // ---- products
     const uint32_t idesc = make_idesc(kRows, 16, 0, 1) + ((uint32_t)((a.d_h >> 3) - 2) << 17);
     constexpr uint32_t hi_sw = desc_hi(1024, 2);
@@ -1157,47 +1191,47 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
       }
     }
   } else {
-    // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 16 p
+    // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 32 p
+    constexpr int kP = kRows / (2 * kUpWarps);
     const int col4 = tid & 15, row_t = tid >> 4;
-    int u = 0;
+    int slot = 0;
+    uint32_t turn = 0;
     for (int q = 0; q < mine; ++q) {
       const int st = q & 1;
       const bool in = (c0 + q) * 64 + col4 * 4 < a.vw;
-      float4 acc[8];
+      float4 acc[kP];
 #pragma unroll
-      for (int p = 0; p < 8; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < steps; ++k, ++u) {
-        const int slot = u % a.n_slots;
-        ok = ok && mbar_wait(smem_u32(&bars->full[slot]), (u / a.n_slots) & 1, s_abort, 5);
-        if (ok) {
-          const unsigned char* const src = s_ring + (size_t)slot * a.slot_bytes + col4 * 16;
+      for (int p = 0; p < kP; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int k = 0; k < steps; ++k) {
+        ok = ok && mbar_wait(smem_u32(&bars->full[slot]), turn, s_abort, 5);
+        const unsigned char* src = s_ring + (size_t)slot * a.slot_bytes + col4 * 16;
+#pragma unroll 1
+        for (int g = 0; g < a.group && k * a.group + g < most; ++g, src += n_rows * 256) {
+          float w[kP];
+          float4 x[kP];
 #pragma unroll
-          for (int p = 0; p < 8; ++p) {
-            const int row = row_t + 16 * p;
-            if (row >= n_rows) continue;
-            float w;
-            if (k < kUpHeld) {
-              w = s_wt[row * kUpHeld + k];
-            } else {
-              w = k < s_run[row].y ? exp2f(__ldcg(a.part_ml + ((long long)(s_run[row].x + k) * a.n_half + half) * kRows + hr + row % a.m).x - s_ml[row].x) * s_ml[row].y : 0.f;
-            }
-            if (w != 0.f && in) {          // (a weight of zero keeps out what a row without a sum holds)
-              const float4 x = *(const float4*)(src + row * 256);
-              acc[p].x = fmaf(x.x, w, acc[p].x); acc[p].y = fmaf(x.y, w, acc[p].y);
-              acc[p].z = fmaf(x.z, w, acc[p].z); acc[p].w = fmaf(x.w, w, acc[p].w);
-            }
+          for (int p = 0; p < kP; ++p) w[p] = in ? weight(row_t + 2 * kUpWarps * p, k * a.group + g) : 0.f;
+#pragma unroll
+          for (int p = 0; p < kP; ++p) x[p] = *(const float4*)(src + min(row_t + 2 * kUpWarps * p, n_rows - 1) * 256);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) {   // (a weight of zero keeps out what a row without a sum holds)
+            acc[p].x = w[p] != 0.f ? fmaf(x[p].x, w[p], acc[p].x) : acc[p].x;
+            acc[p].y = w[p] != 0.f ? fmaf(x[p].y, w[p], acc[p].y) : acc[p].y;
+            acc[p].z = w[p] != 0.f ? fmaf(x[p].z, w[p], acc[p].z) : acc[p].z;
+            acc[p].w = w[p] != 0.f ? fmaf(x[p].w, w[p], acc[p].w) : acc[p].w;
           }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->empty[slot]));
+        if (++slot == a.n_slots) { slot = 0; turn ^= 1; }
       }
       // the products of chunk q - 2 have read the stage
       if (q >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[st]), ((q >> 1) - 1) & 1, s_abort, 6);
       unsigned char* const hi = base + st * 2 * kRows * 128;
 #pragma unroll
-      for (int p = 0; p < 8; ++p) {
-        const int row = row_t + 16 * p;
-        if (row >= n_rows) continue;       // (rows of nobody hold anything)
+      for (int p = 0; p < kP; ++p) {       // (rows of nobody are zeros)
+        const int row = row_t + 2 * kUpWarps * p;
         const float4 v = acc[p];
         const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
         const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
@@ -1218,18 +1252,34 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   tc_fence_after();
   ok = __syncthreads_and(ok) != 0;
 
-  const int quarter = warp & 3, part = warp >> 2;        // rows of a warp; two warps share its columns, 8 at a time
+  const int quarter = warp & 3, part = warp >> 2;        // rows of a warp; kUpWarps / 4 warps share their columns, 8 at a time
+  constexpr int kParts = kUpWarps / 4;
   const int row = quarter * 32 + lane;
   bf16* const dst = a.out + (((long long)b0 * a.m + row) * a.n_h + h) * a.d_h;
   const uint32_t tm = tmem + ((uint32_t)(quarter * 32) << 16);
+  const bool wide = ((uintptr_t)a.out & 15) == 0;        // (rows are whole 32 bytes; the caller's `out` is on 4)
+  auto store8 = [&](bf16* to, const float* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bf162 y = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+      w[e] = *(const uint32_t*)&y;
+    }
+    if (wide) {
+      *(uint4*)to = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ((uint32_t*)to)[e] = w[e];
+    }
+  };
   if (KS == 1) {
-    for (int c = part * 8; c < a.d_h && ok && warp < 8; c += 16) {
-      float v[8];
-      tc_ld8(tm + c, v);
+    for (int c = part * 16; c < a.d_h && ok && warp < kUpWarps; c += 16 * kParts) {
+      float v[16];
+      tc_ld16(tm + c, v);
       tc_wait_ld();
       if (row < n_rows) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) *(bf162*)(dst + c + 2 * e) = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        store8(dst + c, v);
+        store8(dst + c + 8, v + 8);
       }
       __syncwarp();
     }
@@ -1239,27 +1289,28 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     float* const recv = (float*)base;                    // [source][column][row], over stages and ring
     static_assert(kRows * 256 * 4 <= UpSmem::a_bytes + kUpRing - 32 * 1024, "the sums of a tile fit");
     cluster_sync_all();                                  // all bulk copies have landed and all products are done in every block
-    for (int c = part * 8; c < a.d_h && warp < 8; c += 16) {
+    for (int c = part * 8; c < a.d_h && warp < kUpWarps; c += 8 * kParts) {
       float v[8];
       tc_ld8(tm + c, v);
       tc_wait_ld();
+      // (w is a multiple of 8: the columns have one owner)
+      const int q = c / w;
+      const uint32_t to = map_to_cta(smem_u32(recv + ((size_t)z * w + c - q * w) * kRows + row), (uint32_t)q);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int q = (c + e) / w, k = c + e - q * w;
-        st_cluster_u32(map_to_cta(smem_u32(recv + ((size_t)z * w + k) * kRows + row), (uint32_t)q), __float_as_uint(v[e]));
-      }
+      for (int e = 0; e < 8; ++e) st_cluster_u32(to + e * kRows * 4, __float_as_uint(v[e]));
     }
     __syncwarp();
     cluster_sync_all();
-    if (row < n_rows && ok && warp < 8) {
-      for (int k = part * 2; k < w; k += 4) {
-        float s0 = 0.f, s1 = 0.f;
+    if (row < n_rows && ok && warp < kUpWarps) {
+      for (int k = part * 8; k < w; k += 8 * kParts) {
+        float v[8];
 #pragma unroll
-        for (int q = 0; q < KS; ++q) {
-          s0 += recv[((size_t)q * w + k) * kRows + row];
-          s1 += recv[((size_t)q * w + k + 1) * kRows + row];
+        for (int e = 0; e < 8; ++e) {
+          v[e] = recv[(size_t)(k + e) * kRows + row];
+#pragma unroll
+          for (int q = 1; q < KS; ++q) v[e] += recv[((size_t)q * w + k + e) * kRows + row];
         }
-        *(bf162*)(dst + z * w + k) = __floats2bfloat162_rn(s0, s1);
+        store8(dst + z * w + k, v);
       }
     }
   }
@@ -1267,7 +1318,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   __syncthreads();
   if (*s_abort) drain_after_abort();
   if (tid == 0 && *s_abort) ekv_record(a.status, ELITEKV_ERR_TIMEOUT, (int)blockIdx.x | (*s_abort << 16), (int)blockIdx.y);
-  if (warp == 9) {
+  if (warp == kUpWarps + 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
   }
@@ -1505,20 +1556,26 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   u.n_half = s.n_rb * s.cg;
   u.vw = L->vw;
   u.status = L->d_status;
-  u.spt = kRows / c.m;
   u.n_w = UpSmem::n_w(L->d_h);
-  u.slot_bytes = (c.B < u.spt ? c.B : u.spt) * c.m * 256;
-  u.n_slots = UpSmem::ring(L->d_h) / u.slot_bytes < kUpSlots ? UpSmem::ring(L->d_h) / u.slot_bytes : kUpSlots;
-  // shares of the depth: a block takes a step per 64 latents and about four more to start and end
-  const long long groups = (c.B + u.spt - 1) / u.spt, tiles = L->n_h * groups;
-  const int chunks = (L->vw + 63) / 64;
+  // Sequences per tile and shares of the depth: in steps of a whole tile's 64 latents, a block takes one per 64 latents, less
+  // when it has fewer rows, and about four to start and end.
+  const int chunks = (L->vw + 63) / 64, most = kRows / c.m;
   int ks = 1;
-  long long best = 0;
+  float best = 0.f;
   for (int k = 1; k <= 4 && k <= chunks; k *= 2) {
-    if (L->d_h % (4 * k) != 0) break;
-    const long long t = (tiles * k + L->sm_count - 1) / L->sm_count * ((chunks + k - 1) / k + 4);
-    if (k == 1 || t < best) { best = t; ks = k; }
+    if (L->d_h % (8 * k) != 0) break;
+    for (int spt = most; spt >= 1 && spt * 4 >= most; --spt) {
+      const long long tiles = L->n_h * (((long long)c.B + spt - 1) / spt);
+      const float t = (float)((tiles * k + L->sm_count - 1) / L->sm_count) * ((float)((chunks + k - 1) / k) * (0.3f + 0.7f * (float)(spt * c.m) / kRows) + 4.f);
+      if ((k == 1 && spt == most) || t < best) { best = t; ks = k; u.spt = spt; }
+      if (spt > 8) spt = (spt + 1) / 2 + 1;
+    }
   }
+  const int up_rows = (c.B < u.spt ? c.B : u.spt) * c.m;
+  u.group = kRows / up_rows < kUpHeld ? kRows / up_rows : kUpHeld;      // runs that a slot holds
+  u.slot_bytes = u.group * up_rows * 256;
+  u.n_slots = UpSmem::ring(L->d_h) / u.slot_bytes < kUpSlots ? UpSmem::ring(L->d_h) / u.slot_bytes : kUpSlots;
+  const long long groups = ((long long)c.B + u.spt - 1) / u.spt;
   auto launch_up = [&](auto kern) -> int {
     const size_t sm = UpSmem::total(L->d_h);
     EKV_CUDA_OK(ekv_allow_smem(kern, sm));
