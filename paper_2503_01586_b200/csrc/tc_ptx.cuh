@@ -357,9 +357,9 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cbar) {
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cbar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cbar) : "memory");
 }
-// arrival on a barrier of any block of the cluster that also announces bytes to come
-__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cbar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cbar), "r"(bytes) : "memory");
+// arrival on a barrier of any block of the cluster that announces bytes to come, and orders nothing
+__device__ __forceinline__ void mbar_expect_tx_cluster_relaxed(uint32_t cbar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cbar), "r"(bytes) : "memory");
 }
 // probe with acquire at cluster scope: pairs with mbar_arrive_cluster of the peer block
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {

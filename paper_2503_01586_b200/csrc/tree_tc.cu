@@ -551,7 +551,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
         for (int c = 0; c < CG; ++c) {
           const uint32_t cbar = map_to_cta(bar, c);
-          if (lane == 0) mbar_expect_tx_cluster(cbar, 48);
+          if (lane == 0) mbar_expect_tx_cluster_relaxed(cbar, 48);
           if (lane < 3) st_async_v4(map_to_cta(to, c), (uint32_t)x, (uint32_t)y, (uint32_t)z, (uint32_t)t, cbar);
         }
         __syncwarp();
@@ -1015,6 +1015,7 @@ struct UpArgs {
   int B, m, n_h, d_h, hb, n_half, vw, spt, n_w, n_slots, slot_bytes, group;
   int32_t* status;
 };
+template <int N> struct UpRows { static constexpr int value = N; };      // rows of a thread that joins
 struct __align__(16) UpBars {
   uint64_t full[kUpSlots], empty[kUpSlots], a_full[2], done[2], w_full[3];
 };
@@ -1191,59 +1192,74 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
       }
     }
   } else {
-    // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 32 p
-    constexpr int kP = kRows / (2 * kUpWarps);
+    // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 32 p, p < P
     const int col4 = tid & 15, row_t = tid >> 4;
-    int slot = 0;
-    uint32_t turn = 0;
-    for (int q = 0; q < mine; ++q) {
-      const int st = q & 1;
-      const bool in = (c0 + q) * 64 + col4 * 4 < a.vw;
-      float4 acc[kP];
+    constexpr int kStep = 2 * kUpWarps;
+    auto join = [&](auto rows_per_thread) {
+      constexpr int P = decltype(rows_per_thread)::value, U = 4 / P;      // U runs at a time
+      int slot = 0;
+      uint32_t turn = 0;
+      for (int q = 0; q < mine; ++q) {
+        const int st = q & 1;
+        const bool in = (c0 + q) * 64 + col4 * 4 < a.vw;
+        float4 acc[P];
 #pragma unroll
-      for (int p = 0; p < kP; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 0; p < P; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-      for (int k = 0; k < steps; ++k) {
-        ok = ok && mbar_wait(smem_u32(&bars->full[slot]), turn, s_abort, 5);
-        const unsigned char* src = s_ring + (size_t)slot * a.slot_bytes + col4 * 16;
+        for (int k = 0; k < steps; ++k) {
+          ok = ok && mbar_wait(smem_u32(&bars->full[slot]), turn, s_abort, 5);
+          const unsigned char* const src = s_ring + (size_t)slot * a.slot_bytes + col4 * 16;
+          const int n_g = min(a.group, most - k * a.group);
 #pragma unroll 1
-        for (int g = 0; g < a.group && k * a.group + g < most; ++g, src += n_rows * 256) {
-          float w[kP];
-          float4 x[kP];
+          for (int g = 0; g < n_g; g += U) {
+            float w[U][P];
+            float4 x[U][P];
 #pragma unroll
-          for (int p = 0; p < kP; ++p) w[p] = in ? weight(row_t + 2 * kUpWarps * p, k * a.group + g) : 0.f;
+            for (int e = 0; e < U; ++e)
 #pragma unroll
-          for (int p = 0; p < kP; ++p) x[p] = *(const float4*)(src + min(row_t + 2 * kUpWarps * p, n_rows - 1) * 256);
+              for (int p = 0; p < P; ++p) {
+                w[e][p] = in && g + e < n_g ? weight(row_t + kStep * p, k * a.group + g + e) : 0.f;
+                x[e][p] = *(const float4*)(src + (min(g + e, n_g - 1) * n_rows + min(row_t + kStep * p, n_rows - 1)) * 256);
+              }
 #pragma unroll
-          for (int p = 0; p < kP; ++p) {   // (a weight of zero keeps out what a row without a sum holds)
-            acc[p].x = w[p] != 0.f ? fmaf(x[p].x, w[p], acc[p].x) : acc[p].x;
-            acc[p].y = w[p] != 0.f ? fmaf(x[p].y, w[p], acc[p].y) : acc[p].y;
-            acc[p].z = w[p] != 0.f ? fmaf(x[p].z, w[p], acc[p].z) : acc[p].z;
-            acc[p].w = w[p] != 0.f ? fmaf(x[p].w, w[p], acc[p].w) : acc[p].w;
+            for (int e = 0; e < U; ++e)
+#pragma unroll
+              for (int p = 0; p < P; ++p) {          // (a weight of zero keeps out what a row without a sum holds)
+                const float4 y = x[e][p];
+                const float v = w[e][p];
+                acc[p].x = v != 0.f ? fmaf(y.x, v, acc[p].x) : acc[p].x;
+                acc[p].y = v != 0.f ? fmaf(y.y, v, acc[p].y) : acc[p].y;
+                acc[p].z = v != 0.f ? fmaf(y.z, v, acc[p].z) : acc[p].z;
+                acc[p].w = v != 0.f ? fmaf(y.w, v, acc[p].w) : acc[p].w;
+              }
           }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars->empty[slot]));
+          if (++slot == a.n_slots) { slot = 0; turn ^= 1; }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars->empty[slot]));
-        if (++slot == a.n_slots) { slot = 0; turn ^= 1; }
-      }
-      // the products of chunk q - 2 have read the stage
-      if (q >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[st]), ((q >> 1) - 1) & 1, s_abort, 6);
-      unsigned char* const hi = base + st * 2 * kRows * 128;
+        // the products of chunk q - 2 have read the stage
+        if (q >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[st]), ((q >> 1) - 1) & 1, s_abort, 6);
+        unsigned char* const hi = base + st * 2 * kRows * 128;
 #pragma unroll
-      for (int p = 0; p < kP; ++p) {       // (rows of nobody are zeros)
-        const int row = row_t + 2 * kUpWarps * p;
-        const float4 v = acc[p];
-        const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
-        const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
-        const bf162 l0 = __floats2bfloat162_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2bfloat162_rn(v.z - f1.x, v.w - f1.y);
-        const int at = row * 128 + (((col4 >> 1) ^ (row & 7)) << 4) + (col4 & 1) * 8;
-        *(uint2*)(hi + at) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
-        *(uint2*)(hi + kRows * 128 + at) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
+        for (int p = 0; p < P; ++p) {      // (rows of nobody are zeros or hold anything)
+          const int row = row_t + kStep * p;
+          const float4 v = acc[p];
+          const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
+          const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
+          const bf162 l0 = __floats2bfloat162_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2bfloat162_rn(v.z - f1.x, v.w - f1.y);
+          const int at = row * 128 + (((col4 >> 1) ^ (row & 7)) << 4) + (col4 & 1) * 8;
+          *(uint2*)(hi + at) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
+          *(uint2*)(hi + kRows * 128 + at) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->a_full[st]));
       }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars->a_full[st]));
-    }
+    };
+    static_assert(kRows == 4 * kStep, "rows per thread");
+    if (n_rows <= kStep) join(UpRows<1>());
+    else if (n_rows <= 2 * kStep) join(UpRows<2>());
+    else join(UpRows<4>());
     // the last products of both stages
     if (mine >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[mine & 1]), ((mine - 2) >> 1) & 1, s_abort, 7);
     if (mine >= 1) ok = ok && mbar_wait(smem_u32(&bars->done[(mine - 1) & 1]), ((mine - 1) >> 1) & 1, s_abort, 8);
@@ -1344,7 +1360,7 @@ TreeShape tree_shape(const elitekv_layer* L, int m) {
     s.n_rc = steps > s.n_rc ? steps : s.n_rc;
   }
   s.workers = L->sm_count / s.cg;
-  s.want = 4 * s.workers / (s.n_rb * s.n_ct);
+  s.want = 2 * s.workers / (s.n_rb * s.n_ct);
   if (s.want < 1) s.want = 1;
   return s;
 }
