@@ -42,9 +42,11 @@
 namespace {
 
 constexpr int kRows = 128;              // rows per block
-constexpr int kTile = 256;              // tokens of a score unit, latent columns of a value unit
+constexpr int kTile = 256;              // latent columns of a value unit
 constexpr int kPiece = 2048;            // most tokens of a piece
-constexpr int kTiles = kPiece / kTile;
+// Tokens of a score unit.  One block: half as many, because a call of few rows is bound by memory and all units under way
+// should fit L2 until their value units come (148 units of 256 tokens of a 7B cache are 155 MB).
+__host__ __device__ constexpr int score_tile(int cg) { return cg == 2 ? 256 : 128; }
 constexpr int kSlots = 64;              // pieces in the ring
 constexpr int kMostAhead = kSlots - 8;  // D at most
 constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 loads cache rows, 3 clears drafted rows, 4-11 epilogue, 12 claims units
@@ -67,7 +69,7 @@ struct TreeTcArgs {
   int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v, v3;
   float scale_log2e;
   bf16* P;                    // [slot][CG][128][kPiece]
-  float2* stats;              // [slot][CG][tiles][128]: (reference, sum) of a row's 256 tokens
+  float2* stats;              // [slot][CG][tiles][128]: (reference, sum) of a row's tile
   float2* pref;               // [slot][CG][128]: the same of the piece
   float2* cstate;             // [run][rb][ct][CG][128]: of the run so far
   int *s_cnt, *ready, *v_done, *chain;
@@ -172,7 +174,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r,
                const __grid_constant__ CUtensorMap map_ps, const __grid_constant__ CUtensorMap map_o, const TreeTcArgs a) {
   using SM = TreeSmem<CG>;
-  constexpr int NST = SM::n_stages;
+  constexpr int NST = SM::n_stages, TS = score_tile(CG), kTiles = kPiece / TS;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   TreeBars* const bars = (TreeBars*)(base + NST * SM::stage + SM::out);
@@ -245,13 +247,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 1);
       if (!ok) break;
       const volatile TreeUnit* u = s_unit + q_slot();
-      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, n = u->n, gen = u->gen;
+      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, n = u->n;
       const int prefix = n - u->nodes;
       __syncwarp();
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
-        const int all = min(kTile / a.box_s, (n - (tok0 + idx * kTile) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
+        const int all = min(TS / a.box_s, (n - (tok0 + idx * TS) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
         const int h0 = (rb * CG + (int)rank) * a.hb;
         const uint32_t bytes_b = (uint32_t)(all * a.box_s * 128), bytes_l = (uint32_t)(CG * a.m * a.hb * 128) + bytes_b;
         const int yq = ((b * a.n_rb + rb) * CG + (int)rank) * a.n_rc * kRows;
@@ -276,10 +278,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           __syncwarp();
         }
       } else {
-        // P of the piece is complete when each block's rows are
-        ok = __all_sync(0xffffffffu, lane != 0 || poll_global(a.ready + slot, (gen + 1) * CG, s_abort, 3));
-        if (!ok) break;
-        fence_proxy_all();
+        fence_proxy_all();                  // (P of the piece is complete: the unit was published after that)
         const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
         const int ch_all = a.v3 ? kTile / 64 : min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);      // 64-column chunks, both blocks
         const int y = (slot * CG + (int)rank) * kRows;
@@ -316,8 +315,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
-        const int t0 = tok0 + idx * kTile + (CG == 2 ? (int)rank * 128 : 0);
-        const int bs = a.box_s, mine = min(kTile / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
+        const int t0 = tok0 + idx * TS + (int)rank * (TS / CG);
+        const int bs = a.box_s, mine = min(TS / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
         int row = 0;
         if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
         const int xr = tree_rope_col(rb * CG * a.hb, a.r2);
@@ -383,7 +382,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   } else if (warp == 1) {
     // ============================================================== products (the first block's warp, for both)
     if (rank == 0) {
-      constexpr uint32_t idesc_s = make_idesc(kRows * CG, kTile, 0, 0), idesc_v = make_idesc(kRows * CG, kTile, 0, 1);
+      constexpr uint32_t idesc_s = make_idesc(kRows * CG, TS, 0, 0), idesc_v = make_idesc(kRows * CG, kTile, 0, 1);
       constexpr uint32_t hi_sw = desc_hi(1024, 2);
       const uint32_t base16 = (smem_u32(base) >> 4) & 0x3FFFu;
       bool ok = true;
@@ -531,7 +530,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         int n_s = 0, n_v = 0;
         bool stop = false;
         for (;;) {
-          n_s = j < n_pieces ? (walk_len(ws) + kTile - 1) / kTile : 0;
+          n_s = j < n_pieces ? (walk_len(ws) + TS - 1) / TS : 0;
           n_v = j >= ahead ? a.n_ct : 0;
           stop = j >= n_pieces + ahead;
           if (stop || unit < first + n_s + n_v) break;
@@ -543,6 +542,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const int at = unit - first;
         const bool score = at < n_s;
         const PieceWalk& w = score ? ws : wv;
+        // a value unit is published when P of its piece is complete, in both blocks' rows
+        if (!stop && !score && !__all_sync(0xffffffffu, lane != 0 || poll_global(a.ready + w.p % kSlots, (w.p / kSlots + 1) * CG, s_abort, 3))) break;
         int x, y, z, t;                        // 16 bytes of the unit per lane
         if (lane == 0) { x = stop ? kStop : score ? kScore : kValue; y = w.r.x; z = w.rb; t = w.r.y + w.k * kPiece; }
         else if (lane == 1) { x = walk_len(w); y = score ? at : at - n_s; z = w.p % kSlots; t = w.p / kSlots; }
@@ -617,13 +618,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (lane == 0) arrive_read(smem_u32(&bars->acc_empty[group_id]));
       };
       if (type == kScore) {
-        const int t0 = tok0 + idx * kTile;
+        const int t0 = tok0 + idx * TS;
         // the slot's last piece is read to the end
         if (gen > 0 && !group([&]() { return poll_global(a.v_done + slot, gen * a.n_ct * CG, s_abort, 13); })) break;
         if (!group_bar(acc_bar, acc_par, 14)) break;
         tc_fence_after();
         // which of 32 tokens the row sees; tiles of committed tokens alone skip it
-        const bool all = t0 + kTile <= prefix;
+        const bool all = t0 + TS <= prefix;
         auto seen_bits = [&](int t) -> unsigned {                  // tokens t .. t + 31
           if (t + 32 <= prefix) return 0xffffffffu;
           const int d = prefix - t;                                // committed ones in front: d of them
@@ -661,19 +662,19 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              tma_store_2d(&map_ps, idx * kTile + cc * 32, (int)half * kRows + quarter * 32, out_box + (cc & 1) * (kOutBytes / 2));
+              tma_store_2d(&map_ps, idx * TS + cc * 32, (int)half * kRows + quarter * 32, out_box + (cc & 1) * (kOutBytes / 2));
               bulk_commit_group();
             }
           };
           float v0[32], v1[32];
           tc_ld32(tm, v0);
 #pragma unroll 1
-          for (int cc = 0; cc < kTile / 32; cc += 2) {
+          for (int cc = 0; cc < TS / 32; cc += 2) {
             tc_wait_ld();
             tc_ld32(tm + (cc + 1) * 32, v1);
             chunk(cc, v0);
             tc_wait_ld();
-            if (cc + 2 < kTile / 32) tc_ld32(tm + (cc + 2) * 32, v0);
+            if (cc + 2 < TS / 32) tc_ld32(tm + (cc + 2) * 32, v0);
             chunk(cc + 1, v1);
           }
           sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
@@ -695,7 +696,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
         __threadfence();
         named_bar_sync(2 + group_id, kEpiThreads);
-        const int tiles = (len + kTile - 1) / kTile;
+        const int tiles = (len + TS - 1) / TS;
         if (leader) {
           const int before = atomicAdd(a.s_cnt + half, 1);
           __threadfence();
@@ -718,9 +719,9 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const float f = x[t].x == m_ref ? 1.f : exp2f(x[t].x - m_ref);
             total = fmaf(x[t].y, f, total);
             if (f != 1.f && real) {
-              uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * kTile);
+              uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * TS);
 #pragma unroll 1
-              for (int e = 0; e < kTile / 2; ++e) {
+              for (int e = 0; e < TS / 2; ++e) {
                 const uint32_t w = __ldcg(pr + e);
                 const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
                 pr[e] = *(const uint32_t*)&y;
@@ -842,7 +843,7 @@ struct TreePrepArgs {
   const int32_t *seq_lens, *n_nodes;
   const bf16* q_rope;
   bf16* qr;                   // [B][row block][block][n_rc][128][64]
-  int B, m, n_rb, n_ct, want, workers, cg, n_h, r2, hb, n_rc, zero_blocks;
+  int B, m, n_rb, n_ct, ts, want, workers, cg, n_h, r2, hb, n_rc, zero_blocks;
   long long max_len;
   int* hdr;
   int4* runs;
@@ -948,7 +949,7 @@ tree_prep_kernel(const TreePrepArgs a) {
       t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
       cut(t, runs, len, pieces, last);
     }
-    const int items = runs > 0 ? (runs - 1) * pieces + last : 0, scores = runs > 0 ? (t.n + 255) / 256 : 0;
+    const int items = runs > 0 ? (runs - 1) * pieces + last : 0, scores = runs > 0 ? (t.n + a.ts - 1) / a.ts : 0;
     int v[3] = {runs, items, scores}, x[3];
 #pragma unroll
     for (int e = 0; e < 3; ++e) {
@@ -1001,8 +1002,8 @@ tree_prep_kernel(const TreePrepArgs a) {
 // distributed shared memory.
 // Bound: the partial results, read once; the ring keeps up to 96 KB of them in flight (32 KB, in registers, took 3 times
 // as long).
-constexpr int kUpWarps = 16;              // that join and lay out; one more for partial results, one for products and W_uv
-constexpr int kUpThreads = 32 * (kUpWarps + 2);
+constexpr int kUpWarps = 16;              // that join and lay out; one more each for partial results, products, W_uv
+constexpr int kUpThreads = 32 * (kUpWarps + 3);
 constexpr int kUpSlots = 16;              // of the ring, at most
 constexpr int kUpRing = 96 * 1024;
 constexpr int kUpHeld = 8;                // runs whose weights a row keeps
@@ -1017,7 +1018,7 @@ struct UpArgs {
 };
 template <int N> struct UpRows { static constexpr int value = N; };      // rows of a thread that joins
 struct __align__(16) UpBars {
-  uint64_t full[kUpSlots], empty[kUpSlots], a_full[2], done[2], w_full[3];
+  uint64_t full[kUpSlots], empty[kUpSlots], a_full[2], done[2], w_full[3], w_empty[3];
 };
 struct UpSmem {
   static constexpr int a_bytes = 2 * 2 * kRows * 128;                 // 2 stages of head and remainder
@@ -1057,7 +1058,10 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
       mbar_init(smem_u32(&bars->a_full[i]), kUpWarps);
       mbar_init(smem_u32(&bars->done[i]), 1);
     }
-    for (int i = 0; i < 3; ++i) mbar_init(smem_u32(&bars->w_full[i]), 1);
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(smem_u32(&bars->w_full[i]), 1);
+      mbar_init(smem_u32(&bars->w_empty[i]), 1);
+    }
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
@@ -1182,14 +1186,16 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
           tc_mma_w(tmem, la + (kRows * 128 >> 4) + 2 * k, hi_sw, lb + 128 * k, hi_sw, idesc, 1);
         }
         tc_commit(smem_u32(&bars->done[st]));
+        tc_commit(smem_u32(&bars->w_empty[q % a.n_w]));
       }
       __syncwarp();
-      // the W_uv block after the next goes where the products before these read theirs
-      if (q + a.n_w - 1 < mine) {
-        if (q > 0) ok = warp_wait(smem_u32(&bars->done[st ^ 1]), ((q - 1) >> 1) & 1, s_abort, 4);
-        if (ok && lane == 0) load_w(q + a.n_w - 1);
-        __syncwarp();
-      }
+    }
+  } else if (warp == kUpWarps + 2) {
+    // ---- W_uv: a block goes where the products n_w chunks before read theirs
+    for (int q = a.n_w - 1; q < mine && ok; ++q) {
+      if (q >= a.n_w) ok = warp_wait(smem_u32(&bars->w_empty[q % a.n_w]), (q / a.n_w - 1) & 1, s_abort, 4);
+      if (ok && lane == 0) load_w(q);
+      __syncwarp();
     }
   } else {
     // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 32 p, p < P
@@ -1379,7 +1385,7 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.first = o;  o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
   c.n_zero = (size_t)kSlots * (s.cg + 2) + chains;
   c.zero = o;   o = align256(o + sizeof(int) * c.n_zero);
-  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * kTiles * kRows);
+  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * (kPiece / score_tile(s.cg)) * kRows);
   c.pref = o;   o = align256(o + sizeof(float2) * kSlots * s.cg * kRows);
   c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * kRows);
   c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
@@ -1513,6 +1519,7 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   p.q_rope = (const bf16*)c.q_rope;
   p.qr = (bf16*)(base + w.qr);
   p.cg = s.cg;
+  p.ts = score_tile(s.cg);
   p.n_h = L->n_h;
   p.r2 = a.r2;
   p.hb = s.hb;
