@@ -68,7 +68,8 @@ struct TreeTcArgs {
   const uint64_t* mask;
   int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v, v3;
   float scale_log2e;
-  bf16* P;                    // [slot][CG][128][kPiece]
+  bf16* P;                    // [slot][CG][kPiece / 64][128][64]: what a step loads is one piece (4 KB from row to row: 655 clocks a
+                              // step instead of 530)
   float2* stats;              // [slot][CG][tiles][128]: (reference, sum) of a row's tile
   float2* pref;               // [slot][CG][128]: the same of the piece
   float2* cstate;             // [run][rb][ct][CG][128]: of the run so far
@@ -281,7 +282,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         fence_proxy_all();                  // (P of the piece is complete: the unit was published after that)
         const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
         const int ch_all = a.v3 ? kTile / 64 : min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);      // 64-column chunks, both blocks
-        const int y = (slot * CG + (int)rank) * kRows;
+        const int y = (slot * CG + (int)rank) * (kPiece / 64) * kRows;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int t0 = tok0 + ks * 64, boxes = min(per, (n - t0 + bv - 1) / bv);
           const bool special = t0 + 64 > prefix;
@@ -294,7 +295,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           __syncwarp();
           if (elect_one()) {
             if (rank == 0) mbar_expect_tx(fb, (uint32_t)(CG * kABytes + (special ? 0 : ch_all * boxes * bv * 128)));
-            if (CG == 2) tma_load_2d_pair(dst, &map_p, ks * 64, y, cfb); else tma_load_2d(dst, &map_p, ks * 64, y, cfb);
+            if (CG == 2) tma_load_2d_pair(dst, &map_p, 0, y + ks * kRows, cfb); else tma_load_2d(dst, &map_p, 0, y + ks * kRows, cfb);
           }
           __syncwarp();
         }
@@ -662,7 +663,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              tma_store_2d(&map_ps, idx * TS + cc * 32, (int)half * kRows + quarter * 32, out_box + (cc & 1) * (kOutBytes / 2));
+              tma_store_2d(&map_ps, (cc & 1) * 32, ((int)half * (kPiece / 64) + idx * (TS / 64) + (cc >> 1)) * kRows + quarter * 32,
+                           out_box + (cc & 1) * (kOutBytes / 2));
               bulk_commit_group();
             }
           };
@@ -719,12 +721,12 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const float f = x[t].x == m_ref ? 1.f : exp2f(x[t].x - m_ref);
             total = fmaf(x[t].y, f, total);
             if (f != 1.f && real) {
-              uint32_t* const pr = (uint32_t*)(a.P + (half * kRows + r) * kPiece + t * TS);
 #pragma unroll 1
               for (int e = 0; e < TS / 2; ++e) {
-                const uint32_t w = __ldcg(pr + e);
+                uint32_t* const pr = (uint32_t*)(a.P + ((half * (kPiece / 64) + t * (TS / 64) + (e >> 5)) * kRows + r) * 64) + (e & 31);
+                const uint32_t w = __ldcg(pr);
                 const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
-                pr[e] = *(const uint32_t*)&y;
+                *pr = *(const uint32_t*)&y;
               }
             }
           }
@@ -1497,6 +1499,7 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.status = L->d_status;
   CUtensorMap m_q, m_k, m_v, m_p, m_qr, m_r, m_ps, m_o, m_w;
   a.v3 = a.box_v == 64 && L->vw % 64 == 0;
+  const unsigned long long p_rows = (unsigned long long)kSlots * s.cg * (kPiece / 64) * kRows;
   const unsigned long long blk_rows = (unsigned long long)w.max_runs * s.n_rb * s.cg * ((L->vw + 63) / 64) * kRows;
   const unsigned long long rows = plane_rows(cv);
   int rc = make_map_queries(&m_q, c.q_abs, c.B, c.m, L->n_h, L->kw, s.hb);
@@ -1504,10 +1507,10 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   if (rc == ELITEKV_OK)
     rc = a.v3 ? make_map_chunks(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, 4 / s.cg)
               : make_map_pitch(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, a.box_v);
-  if (rc == ELITEKV_OK) rc = make_map_box(&m_ps, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, 2);
+  if (rc == ELITEKV_OK) rc = make_map_box(&m_ps, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.P, p_rows, 64, 2);
   if (rc == ELITEKV_OK) rc = make_map_box(&m_o, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a.part_acc, blk_rows, 64, 4);
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_w, L->d_Wuv, L->vw, (unsigned long long)L->n_h * L->d_h, (unsigned long long)L->n_h * L->d_h, 64);
-  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, (unsigned long long)kSlots * s.cg * kRows, kPiece, kPiece, kRows);
+  if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, p_rows, 64, 64, kRows);
   // (a layer without rope has neither; the maps are not used)
   m_qr = m_r = m_p;
   if (rc == ELITEKV_OK && s.n_rc > 0) {
