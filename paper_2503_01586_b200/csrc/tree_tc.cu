@@ -53,9 +53,9 @@ constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 
 constexpr int kEpiThreads = 128;         // a group of four epilogue warps
 constexpr int kQueue = 4;               // two units with the epilogue groups, two ahead (more would be late for those that wait for them)
 constexpr int kLead = 16;                // steps before a unit's last load at which the next unit is claimed
-constexpr int kMaxStages = 6;
+constexpr int kMaxStages = 5;
 constexpr int kABytes = kRows * 128;
-constexpr int kOutBytes = 4096;         // rows on their way out, per epilogue warp
+constexpr int kOutBytes = 8192;         // rows on their way out, per epilogue warp: two boxes of 32 rows x 128 bytes
 
 enum { kScore = 0, kValue = 1, kStop = 2 };
 
@@ -91,7 +91,7 @@ template <int CG>
 struct TreeSmem {
   static constexpr int b_bytes = kTile / CG * 128;            // 256 (128) token rows, or 64 tokens of 256 (128) columns
   static constexpr int stage = kABytes + b_bytes;
-  static constexpr int n_stages = CG == 2 ? 6 : 4;
+  static constexpr int n_stages = CG == 2 ? 5 : 3;            // (one more: 0.5 % and 3 % with the epilogue's boxes at half their size)
   static constexpr int out = 8 * kOutBytes;
   static constexpr int misc = sizeof(TreeBars) + kQueue * sizeof(TreeUnit) + kQueue * 16 + 64;
   static constexpr int total = n_stages * stage + out + misc + 1024;
@@ -571,11 +571,11 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const int hl = r / a.m, i = r - hl * a.m;
     volatile int* const verdict = s_verdict + 2 * group_id;
     volatile int* const last = s_last + group_id;
-    // rows on their way out: two boxes of 32 rows x 64 bytes per warp (64-byte swizzle)
+    // rows on their way out: two boxes (128-byte swizzle)
     const uint32_t out_box = smem_u32(base + NST * SM::stage + (warp - 4) * kOutBytes);
     auto put = [&](int box, int j, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {       // 16 bytes of this lane's row
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                   ::"r"(out_box + box * (kOutBytes / 2) + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+                   ::"r"(out_box + box * (kOutBytes / 2) + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
     };
     auto out_free = [&]() {                     // the box of the store before the last has been read
       if (lane == 0) bulk_wait_group_read<1>();
@@ -647,7 +647,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
             for (int e = 4; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], x[e]);
             top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
-            out_free();
+            const int box = (cc >> 1) & 1;                         // 64 tokens each
+            if ((cc & 1) == 0) out_free();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
               uint32_t w[4];
@@ -658,13 +659,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 sum4[2 * (e & 1)] += __uint_as_float(w[e] << 16);
                 sum4[2 * (e & 1) + 1] += __uint_as_float(w[e] & 0xffff0000u);
               }
-              put(cc & 1, g, w[0], w[1], w[2], w[3]);
+              put(box, (cc & 1) * 4 + g, w[0], w[1], w[2], w[3]);
             }
+            if ((cc & 1) == 0) return;
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              tma_store_2d(&map_ps, (cc & 1) * 32, ((int)half * (kPiece / 64) + idx * (TS / 64) + (cc >> 1)) * kRows + quarter * 32,
-                           out_box + (cc & 1) * (kOutBytes / 2));
+              tma_store_2d(&map_ps, 0, ((int)half * (kPiece / 64) + idx * (TS / 64) + (cc >> 1)) * kRows + quarter * 32, out_box + box * (kOutBytes / 2));
               bulk_commit_group();
             }
           };
@@ -780,23 +781,18 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 x[e] += y.x * f_old; x[e + 1] += y.y * f_old; x[e + 2] += y.z * f_old; x[e + 3] += y.w * f_old;
               }
           }
+          const int box = cc & 1;
+          out_free();
 #pragma unroll
-          for (int box = 0; box < 2; ++box) {             // 16 columns each
-            if (col + box * 16 >= a.vw) continue;
-            out_free();
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const float* y = x + box * 16 + 4 * g;
-              put(box, g, __float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-            }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) {
-              const uint32_t from = out_box + box * (kOutBytes / 2);
-              if (k_run == 0 || scaled) tma_store_2d(&map_o, (col & 63) + box * 16, (int)row0 + quarter * 32, from);
-              else tma_add_2d(&map_o, (col & 63) + box * 16, (int)row0 + quarter * 32, from);
-              bulk_commit_group();
-            }
+          for (int g = 0; g < 8; ++g)
+            put(box, g, __float_as_uint(x[4 * g]), __float_as_uint(x[4 * g + 1]), __float_as_uint(x[4 * g + 2]), __float_as_uint(x[4 * g + 3]));
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            const uint32_t from = out_box + box * (kOutBytes / 2);
+            if (k_run == 0 || scaled) tma_store_2d(&map_o, col & 63, (int)row0 + quarter * 32, from);
+            else tma_add_2d(&map_o, col & 63, (int)row0 + quarter * 32, from);
+            bulk_commit_group();
           }
         };
         float v0[32], v1[32];
@@ -1203,43 +1199,55 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     // ---- rows joined and laid out: a thread has 4 of a chunk's columns of the rows row_t + 32 p, p < P
     const int col4 = tid & 15, row_t = tid >> 4;
     constexpr int kStep = 2 * kUpWarps;
+    int least = most;                      // runs that every sequence has
+    for (int k = lane; k < n_rows; k += 32) least = min(least, s_run[k].y);
+    least = __reduce_min_sync(0xffffffffu, least);
     auto join = [&](auto rows_per_thread) {
       constexpr int P = decltype(rows_per_thread)::value, U = 4 / P;      // U runs at a time
+      int off[P];                          // of a row in a run's share of a unit
+#pragma unroll
+      for (int p = 0; p < P; ++p) off[p] = min(row_t + kStep * p, n_rows - 1) * 256 + col4 * 16;
+      const float* const wt = s_wt + row_t * kUpHeld;
       int slot = 0;
       uint32_t turn = 0;
       for (int q = 0; q < mine; ++q) {
         const int st = q & 1;
         const bool in = (c0 + q) * 64 + col4 * 4 < a.vw;
+        // all rows of all runs hold values: nothing has to be kept out
+        const int plain = (c0 + q) * 64 + 64 <= a.vw ? min(least, kUpHeld) : 0;
         float4 acc[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
         for (int k = 0; k < steps; ++k) {
           ok = ok && mbar_wait(smem_u32(&bars->full[slot]), turn, s_abort, 5);
-          const unsigned char* const src = s_ring + (size_t)slot * a.slot_bytes + col4 * 16;
-          const int n_g = min(a.group, most - k * a.group);
+          const unsigned char* src = s_ring + (size_t)slot * a.slot_bytes;
+          const int k0 = k * a.group, n_g = min(a.group, most - k0);
 #pragma unroll 1
-          for (int g = 0; g < n_g; g += U) {
-            float w[U][P];
-            float4 x[U][P];
+          for (int g = 0; g < n_g; g += U, src += U * n_rows * 256) {
+            if (g + U <= n_g && k0 + g + U <= plain) {
 #pragma unroll
-            for (int e = 0; e < U; ++e)
+              for (int e = 0; e < U; ++e)
 #pragma unroll
-              for (int p = 0; p < P; ++p) {
-                w[e][p] = in && g + e < n_g ? weight(row_t + kStep * p, k * a.group + g + e) : 0.f;
-                x[e][p] = *(const float4*)(src + (min(g + e, n_g - 1) * n_rows + min(row_t + kStep * p, n_rows - 1)) * 256);
-              }
+                for (int p = 0; p < P; ++p) {
+                  const float4 y = *(const float4*)(src + e * n_rows * 256 + off[p]);
+                  const float v = wt[kStep * p * kUpHeld + k0 + g + e];
+                  acc[p].x = fmaf(y.x, v, acc[p].x); acc[p].y = fmaf(y.y, v, acc[p].y);
+                  acc[p].z = fmaf(y.z, v, acc[p].z); acc[p].w = fmaf(y.w, v, acc[p].w);
+                }
+            } else {
+#pragma unroll 1
+              for (int e = 0; e < U && g + e < n_g; ++e)
 #pragma unroll
-            for (int e = 0; e < U; ++e)
-#pragma unroll
-              for (int p = 0; p < P; ++p) {          // (a weight of zero keeps out what a row without a sum holds)
-                const float4 y = x[e][p];
-                const float v = w[e][p];
-                acc[p].x = v != 0.f ? fmaf(y.x, v, acc[p].x) : acc[p].x;
-                acc[p].y = v != 0.f ? fmaf(y.y, v, acc[p].y) : acc[p].y;
-                acc[p].z = v != 0.f ? fmaf(y.z, v, acc[p].z) : acc[p].z;
-                acc[p].w = v != 0.f ? fmaf(y.w, v, acc[p].w) : acc[p].w;
-              }
+                for (int p = 0; p < P; ++p) {
+                  const float v = in ? weight(row_t + kStep * p, k0 + g + e) : 0.f;
+                  if (v != 0.f) {          // (else the place may hold anything)
+                    const float4 y = *(const float4*)(src + e * n_rows * 256 + off[p]);
+                    acc[p].x = fmaf(y.x, v, acc[p].x); acc[p].y = fmaf(y.y, v, acc[p].y);
+                    acc[p].z = fmaf(y.z, v, acc[p].z); acc[p].w = fmaf(y.w, v, acc[p].w);
+                  }
+                }
+            }
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&bars->empty[slot]));
@@ -1249,7 +1257,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
         if (q >= 2) ok = ok && mbar_wait(smem_u32(&bars->done[st]), ((q >> 1) - 1) & 1, s_abort, 6);
         unsigned char* const hi = base + st * 2 * kRows * 128;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {      // (rows of nobody are zeros or hold anything)
+        for (int p = 0; p < P; ++p) {      // (rows of nobody hold anything)
           const int row = row_t + kStep * p;
           const float4 v = acc[p];
           const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
@@ -1409,13 +1417,13 @@ int make_map_pitch(CUtensorMap* m, const void* ptr, unsigned long long rows, uns
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
 }
-// [rows][cols], box of 32 rows x 64 bytes, 64-byte swizzle: what the epilogue warps write
+// [rows][cols], box of 32 rows x 128 bytes, 128-byte swizzle: what the epilogue warps write
 int make_map_box(CUtensorMap* m, CUtensorMapDataType type, const void* ptr, unsigned long long rows, unsigned long long cols, unsigned size) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return ELITEKV_ERR_CUDA;
   cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * size};
-  cuuint32_t box[2] = {64 / size, 32}, estr[2] = {1, 1};
-  CUresult r = fn(m, type, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+  cuuint32_t box[2] = {128 / size, 32}, estr[2] = {1, 1};
+  CUresult r = fn(m, type, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
 }
