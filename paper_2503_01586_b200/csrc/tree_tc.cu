@@ -281,7 +281,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       } else {
         fence_proxy_all();                  // (P of the piece is complete: the unit was published after that)
         const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
-        const int ch_all = a.v3 ? kTile / 64 : min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);      // 64-column chunks, both blocks
+        const int ch_all = a.v3 ? kTile / 64 : min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);      // 64-column chunks loaded, both blocks
         const int y = (slot * CG + (int)rank) * (kPiece / 64) * kRows;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int t0 = tok0 + ks * 64, boxes = min(per, (n - t0 + bv - 1) / bv);
@@ -339,9 +339,10 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           }
         }
       } else {
-        const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6, x0 = idx * kTile + (CG == 2 ? (int)rank * 128 : 0);
-        const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
-        const int ch = a.v3 ? 4 / CG : CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;
+        const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
+        // this block's columns: its half of the tile's (a quarter where half of the tile is enough: the product's width is halved)
+        const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6), mine = ch_all <= 2 ? 2 / CG : 4 / CG;
+        const int x0 = idx * kTile + (int)rank * mine * 64, ch = a.v3 ? 4 / CG : max(0, min(mine, ch_all - mine * (int)rank));
         int row = 0;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int b0 = ks * per;                    // first box of the step
@@ -384,6 +385,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     // ============================================================== products (the first block's warp, for both)
     if (rank == 0) {
       constexpr uint32_t idesc_s = make_idesc(kRows * CG, TS, 0, 0), idesc_v = make_idesc(kRows * CG, kTile, 0, 1);
+      constexpr uint32_t idesc_h = make_idesc(kRows * CG, kTile / 2, 0, 1);       // the last tile, where half of it is enough
       constexpr uint32_t hi_sw = desc_hi(1024, 2);
       const uint32_t base16 = (smem_u32(base) >> 4) & 0x3FFFu;
       bool ok = true;
@@ -393,6 +395,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (!ok) break;
         const volatile TreeUnit* u = s_unit + q_slot();
         const int type = u->type, tok0 = u->tok0, len = u->len, prefix = u->n - u->nodes;
+        const bool half_tile = a.vw - u->idx * kTile <= kTile / 2;
         __syncwarp();
         if (lane == 0) release_unit();
         if (type == kStop) break;
@@ -415,7 +418,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           // scores: 64 latents of 256 tokens, K-major; values: 64 tokens of 256 columns, 8 KB from one 64-column chunk to the next
           const uint32_t lb = (base16 + ((st * SM::stage + kABytes) >> 4)) | (type == kScore ? 1u << 16 : (8192u >> 4) << 16);
           const uint32_t step_b = type == kScore ? 2 : 128;
-          const uint32_t idesc = type == kScore ? idesc_s : idesc_v;
+          const uint32_t idesc = type == kScore ? idesc_s : half_tile ? idesc_h : idesc_v;
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -448,7 +451,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       } else {
         const int ks_n = (len + 63) >> 6;
         const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
-        const int ch = CG == 2 ? max(0, min(2, ch_all - 2 * (int)rank)) : ch_all;      // (chunks past the last column are not stored)
+        const int mine = ch_all <= 2 ? 2 / CG : 4 / CG, ch = max(0, min(mine, ch_all - mine * (int)rank));      // (chunks past the last column are not stored)
         unsigned nf_lo = 0, nf_hi = 0;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int t0 = tok0 + ks * 64;
