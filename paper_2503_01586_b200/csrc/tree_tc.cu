@@ -1379,7 +1379,7 @@ TreeShape tree_shape(const elitekv_layer* L, int m) {
     s.n_rc = steps > s.n_rc ? steps : s.n_rc;
   }
   s.workers = L->sm_count / s.cg;
-  s.want = 2 * s.workers / (s.n_rb * s.n_ct);
+  s.want = s.workers / (s.n_rb * s.n_ct);
   if (s.want < 1) s.want = 1;
   return s;
 }
