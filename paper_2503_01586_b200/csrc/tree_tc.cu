@@ -42,11 +42,9 @@
 namespace {
 
 constexpr int kRows = 128;              // rows per block
-constexpr int kTile = 256;              // latent columns of a value unit
+constexpr int kTile = 256;              // tokens of a score unit, latent columns of a value unit
 constexpr int kPiece = 2048;            // most tokens of a piece
-// Tokens of a score unit.  One block: half as many, because a call of few rows is bound by memory and all units under way
-// should fit L2 until their value units come (148 units of 256 tokens of a 7B cache are 155 MB).
-__host__ __device__ constexpr int score_tile(int cg) { return cg == 2 ? 256 : 128; }
+constexpr int kTiles = kPiece / kTile;
 constexpr int kSlots = 64;              // pieces in the ring
 constexpr int kMostAhead = kSlots - 8;  // D at most
 constexpr int kTreeThreads = 416;       // warp 0 loads queries and P, 1 MMA, 2 loads cache rows, 3 clears drafted rows, 4-11 epilogue, 12 claims units
@@ -175,7 +173,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r,
                const __grid_constant__ CUtensorMap map_ps, const __grid_constant__ CUtensorMap map_o, const TreeTcArgs a) {
   using SM = TreeSmem<CG>;
-  constexpr int NST = SM::n_stages, TS = score_tile(CG), kTiles = kPiece / TS;
+  constexpr int NST = SM::n_stages;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   TreeBars* const bars = (TreeBars*)(base + NST * SM::stage + SM::out);
@@ -254,7 +252,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
-        const int all = min(TS / a.box_s, (n - (tok0 + idx * TS) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
+        const int all = min(kTile / a.box_s, (n - (tok0 + idx * kTile) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
         const int h0 = (rb * CG + (int)rank) * a.hb;
         const uint32_t bytes_b = (uint32_t)(all * a.box_s * 128), bytes_l = (uint32_t)(CG * a.m * a.hb * 128) + bytes_b;
         const int yq = ((b * a.n_rb + rb) * CG + (int)rank) * a.n_rc * kRows;
@@ -316,8 +314,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
-        const int t0 = tok0 + idx * TS + (int)rank * (TS / CG);
-        const int bs = a.box_s, mine = min(TS / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
+        const int t0 = tok0 + idx * kTile + (int)rank * (kTile / CG);
+        const int bs = a.box_s, mine = min(kTile / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
         int row = 0;
         if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
         const int xr = tree_rope_col(rb * CG * a.hb, a.r2);
@@ -384,7 +382,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   } else if (warp == 1) {
     // ============================================================== products (the first block's warp, for both)
     if (rank == 0) {
-      constexpr uint32_t idesc_s = make_idesc(kRows * CG, TS, 0, 0), idesc_v = make_idesc(kRows * CG, kTile, 0, 1);
+      constexpr uint32_t idesc_s = make_idesc(kRows * CG, kTile, 0, 0), idesc_v = make_idesc(kRows * CG, kTile, 0, 1);
       constexpr uint32_t idesc_h = make_idesc(kRows * CG, kTile / 2, 0, 1);       // the last tile, where half of it is enough
       constexpr uint32_t hi_sw = desc_hi(1024, 2);
       const uint32_t base16 = (smem_u32(base) >> 4) & 0x3FFFu;
@@ -534,7 +532,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         int n_s = 0, n_v = 0;
         bool stop = false;
         for (;;) {
-          n_s = j < n_pieces ? (walk_len(ws) + TS - 1) / TS : 0;
+          n_s = j < n_pieces ? (walk_len(ws) + kTile - 1) / kTile : 0;
           n_v = j >= ahead ? a.n_ct : 0;
           stop = j >= n_pieces + ahead;
           if (stop || unit < first + n_s + n_v) break;
@@ -622,13 +620,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (lane == 0) arrive_read(smem_u32(&bars->acc_empty[group_id]));
       };
       if (type == kScore) {
-        const int t0 = tok0 + idx * TS;
+        const int t0 = tok0 + idx * kTile;
         // the slot's last piece is read to the end
         if (gen > 0 && !group([&]() { return poll_global(a.v_done + slot, gen * a.n_ct * CG, s_abort, 13); })) break;
         if (!group_bar(acc_bar, acc_par, 14)) break;
         tc_fence_after();
         // which of 32 tokens the row sees; tiles of committed tokens alone skip it
-        const bool all = t0 + TS <= prefix;
+        const bool all = t0 + kTile <= prefix;
         auto seen_bits = [&](int t) -> unsigned {                  // tokens t .. t + 31
           if (t + 32 <= prefix) return 0xffffffffu;
           const int d = prefix - t;                                // committed ones in front: d of them
@@ -668,19 +666,19 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              tma_store_2d(&map_ps, 0, ((int)half * (kPiece / 64) + idx * (TS / 64) + (cc >> 1)) * kRows + quarter * 32, out_box + box * (kOutBytes / 2));
+              tma_store_2d(&map_ps, 0, ((int)half * (kPiece / 64) + idx * (kTile / 64) + (cc >> 1)) * kRows + quarter * 32, out_box + box * (kOutBytes / 2));
               bulk_commit_group();
             }
           };
           float v0[32], v1[32];
           tc_ld32(tm, v0);
 #pragma unroll 1
-          for (int cc = 0; cc < TS / 32; cc += 2) {
+          for (int cc = 0; cc < kTile / 32; cc += 2) {
             tc_wait_ld();
             tc_ld32(tm + (cc + 1) * 32, v1);
             chunk(cc, v0);
             tc_wait_ld();
-            if (cc + 2 < TS / 32) tc_ld32(tm + (cc + 2) * 32, v0);
+            if (cc + 2 < kTile / 32) tc_ld32(tm + (cc + 2) * 32, v0);
             chunk(cc + 1, v1);
           }
           sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
@@ -702,7 +700,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
         __threadfence();
         named_bar_sync(2 + group_id, kEpiThreads);
-        const int tiles = (len + TS - 1) / TS;
+        const int tiles = (len + kTile - 1) / kTile;
         if (leader) {
           const int before = atomicAdd(a.s_cnt + half, 1);
           __threadfence();
@@ -726,8 +724,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             total = fmaf(x[t].y, f, total);
             if (f != 1.f && real) {
 #pragma unroll 1
-              for (int e = 0; e < TS / 2; ++e) {
-                uint32_t* const pr = (uint32_t*)(a.P + ((half * (kPiece / 64) + t * (TS / 64) + (e >> 5)) * kRows + r) * 64) + (e & 31);
+              for (int e = 0; e < kTile / 2; ++e) {
+                uint32_t* const pr = (uint32_t*)(a.P + ((half * (kPiece / 64) + t * (kTile / 64) + (e >> 5)) * kRows + r) * 64) + (e & 31);
                 const uint32_t w = __ldcg(pr);
                 const bf162 y = __floats2bfloat162_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
                 *pr = *(const uint32_t*)&y;
@@ -844,7 +842,7 @@ struct TreePrepArgs {
   const int32_t *seq_lens, *n_nodes;
   const bf16* q_rope;
   bf16* qr;                   // [B][row block][block][n_rc][128][64]
-  int B, m, n_rb, n_ct, ts, want, workers, cg, n_h, r2, hb, n_rc, zero_blocks;
+  int B, m, n_rb, n_ct, want, workers, cg, n_h, r2, hb, n_rc, zero_blocks;
   long long max_len;
   int* hdr;
   int4* runs;
@@ -950,7 +948,7 @@ tree_prep_kernel(const TreePrepArgs a) {
       t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
       cut(t, runs, len, pieces, last);
     }
-    const int items = runs > 0 ? (runs - 1) * pieces + last : 0, scores = runs > 0 ? (t.n + a.ts - 1) / a.ts : 0;
+    const int items = runs > 0 ? (runs - 1) * pieces + last : 0, scores = runs > 0 ? (t.n + kTile - 1) / kTile : 0;
     int v[3] = {runs, items, scores}, x[3];
 #pragma unroll
     for (int e = 0; e < 3; ++e) {
@@ -984,8 +982,9 @@ tree_prep_kernel(const TreePrepArgs a) {
   if (tid == 0) {
     a.seq_first[a.B] = run0;
     const long long pieces = (long long)item0 * a.n_rb, units = (long long)score0 * a.n_rb + pieces * a.n_ct;
-    // how far the score units go ahead of the value units: what the workers hold two and a half times over
-    long long d = units > 0 ? (5ll * a.workers * pieces + 2 * units - 1) / (2 * units) : 1;
+    // how far the score units go ahead of the value units: what the workers hold three and a half times over (1.5 times: 3 to 6 %
+    // slower, 2.5: up to 2 %)
+    long long d = units > 0 ? (7ll * a.workers * pieces + 2 * units - 1) / (2 * units) : 1;
     d = d < 1 ? 1 : d > kMostAhead ? kMostAhead : d;
     a.hdr[0] = 0;
     a.hdr[1] = run0;
@@ -1398,7 +1397,7 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.first = o;  o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
   c.n_zero = (size_t)kSlots * (s.cg + 2) + chains;
   c.zero = o;   o = align256(o + sizeof(int) * c.n_zero);
-  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * (kPiece / score_tile(s.cg)) * kRows);
+  c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * kTiles * kRows);
   c.pref = o;   o = align256(o + sizeof(float2) * kSlots * s.cg * kRows);
   c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * kRows);
   c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
@@ -1533,7 +1532,6 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   p.q_rope = (const bf16*)c.q_rope;
   p.qr = (bf16*)(base + w.qr);
   p.cg = s.cg;
-  p.ts = score_tile(s.cg);
   p.n_h = L->n_h;
   p.r2 = a.r2;
   p.hb = s.hb;
