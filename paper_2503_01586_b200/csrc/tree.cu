@@ -6,14 +6,17 @@
 // Node i sees every committed token (t < n - nodes) and the nodes j of its mask (t = n - nodes + j).
 //
 // tree_generic_kernel: a warp per (sequence, node, head) and split of the tokens.  Lanes hold the latent axis, eight
-// coordinates at a time; queries and the running sum (fp32) lie in shared memory.  Tokens that the row does not see
-// are skipped, so that nothing of theirs is read.  Bound: the warp-wide sum of every token (latency), a row's own
-// read of the whole cache (L2).  It serves what the tensor-core form does not cover.
+// coordinates at a time, of four tokens; queries and the running sum (fp32) lie in shared memory.  Tokens that the row does
+// not see are skipped: nothing of theirs is read.  Bound: the trips to L2 of four tokens in turn, a row's own read of the
+// whole cache.  It serves what the tensor-core form does not cover, and calls so small that that form's start costs more.
 #include "tree.cuh"
 
 namespace {
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int kAhead = 4;             // tokens of a warp in flight
+constexpr int kSplits = 32;           // partial results of a row, at most
 
 struct GenArgs {
   const bf16 *q_rope, *q_abs, *rope, *latent;
@@ -61,41 +64,86 @@ __global__ void tree_generic_kernel(const GenArgs a) {
   for (int k = lane; k < a.vw; k += 32) s_acc[k] = 0.f;
   __syncwarp();
   float m_run = -1e30f, l_run = 0.f;
-  for (int t = t0; t < t1; ++t) {
-    if (t >= prefix && !(mask >> (t - prefix) & 1)) continue;
-    int code, detail;
-    long long at = ekv_token_row(a.cv, b, t, &code, &detail);
-    if (at < 0) {
-      if (lane == 0) ekv_record(a.status, code, b, detail);
-      at = 0;                                  // page 0, as in the other attention kernels
+  auto unpack = [](const uint4& x, float* f) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 y = __bfloat1622float2(*(const bf162*)&w[e]);
+      f[2 * e] = y.x;
+      f[2 * e + 1] = y.y;
     }
-    const bf16* c = a.latent + at * a.d_c;
-    float s = 0.f;
+  };
+  for (int t = t0; t < t1; t += kAhead) {
+    bool seen[kAhead];
+    const bf16* c[kAhead];
+    const bf16* kr[kAhead];
+    float s[kAhead];
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) {
+      const int tg = t + g;
+      seen[g] = tg < t1 && (tg < prefix || (mask >> (tg - prefix) & 1));
+      s[g] = 0.f;
+      long long at = 0;
+      if (seen[g]) {
+        int code, detail;
+        at = ekv_token_row(a.cv, b, tg, &code, &detail);
+        if (at < 0) {
+          if (lane == 0) ekv_record(a.status, code, b, detail);
+          at = 0;                                  // page 0, as in the other attention kernels
+        }
+      }
+      c[g] = a.latent + at * a.d_c;
+      kr[g] = a.rope + (at * a.n_h + h) * a.r2;
+    }
     for (int k = lane * 8; k < a.kw; k += 256) {
-      const uint4 x = __ldg((const uint4*)(c + k));
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      uint4 x[kAhead];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = __bfloat1622float2(*(const bf162*)&w[e]);
-        s = fmaf(f.x, s_q[k + 2 * e], s);
-        s = fmaf(f.y, s_q[k + 2 * e + 1], s);
+      for (int g = 0; g < kAhead; ++g) x[g] = seen[g] ? __ldg((const uint4*)(c[g] + k)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) {
+        float f[8];
+        unpack(x[g], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[g] = fmaf(f[e], s_q[k + e], s[g]);
       }
     }
-    for (int k = lane; k < a.r2; k += 32)
-      s = fmaf(__bfloat162float(a.q_rope[row * a.r2 + k]), __bfloat162float(a.rope[(at * a.n_h + h) * a.r2 + k]), s);
-    s = warp_sum(s) * a.scale_log2e;
-    const float m_new = fmaxf(m_run, s), corr = exp2f(m_run - m_new), p = exp2f(s - m_new);
-    l_run = fmaf(l_run, corr, p);
-    m_run = m_new;
-    for (int k = lane * 8; k < a.vw; k += 256) {
-      const uint4 x = __ldg((const uint4*)(c + a.voff + k));
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    for (int k = lane; k < a.r2; k += 32) {
+      const float q = __bfloat162float(a.q_rope[row * a.r2 + k]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = __bfloat1622float2(*(const bf162*)&w[e]);
-        s_acc[k + 2 * e] = fmaf(p, f.x, s_acc[k + 2 * e] * corr);
-        s_acc[k + 2 * e + 1] = fmaf(p, f.y, s_acc[k + 2 * e + 1] * corr);
+      for (int g = 0; g < kAhead; ++g)
+        if (seen[g]) s[g] = fmaf(q, __bfloat162float(kr[g][k]), s[g]);
+    }
+    float m_new = m_run;
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) {
+      s[g] = warp_sum(s[g]) * a.scale_log2e;
+      if (seen[g]) m_new = fmaxf(m_new, s[g]);
+    }
+    const float corr = exp2f(m_run - m_new);
+    m_run = m_new;
+    l_run *= corr;
+    float p[kAhead];
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) {
+      p[g] = seen[g] ? exp2f(s[g] - m_new) : 0.f;
+      l_run += p[g];
+    }
+    for (int k = lane * 8; k < a.vw; k += 256) {
+      uint4 x[kAhead];
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) x[g] = seen[g] ? __ldg((const uint4*)(c[g] + a.voff + k)) : make_uint4(0, 0, 0, 0);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = s_acc[k + e] * corr;
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) {
+        float f[8];
+        unpack(x[g], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = fmaf(p[g], f[e], y[e]);
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s_acc[k + e] = y[e];
     }
   }
   __syncwarp();
@@ -107,11 +155,23 @@ __global__ void tree_generic_kernel(const GenArgs a) {
   }
 }
 
-// Splits: enough warps for the device, at most 16 partial results a row
+// Splits: enough warps for the device
 int generic_splits(const elitekv_layer* L, int B, int m) {
   const long long rows = (long long)B * m * L->n_h, want = 16ll * L->sm_count;
   const long long s = (want + rows - 1) / rows;
-  return (int)(s > 16 ? 16 : s);
+  return (int)(s > kSplits ? kSplits : s);
+}
+
+// Whether a call is so small that the generic kernel is the quicker one.  Its time is the groups of kAhead tokens that
+// a warp takes in turn, each a few trips to L2 and shuffles (about 2 us) and its share of the row; that of the
+// tensor-core form hardly depends on so little work (30 to 52 us).  Measured, generic and tensor-core in us, by groups:
+// rows of 64 latents 1: 15/32, 3: 24/32, 5: 25 to 30/32 to 35, 7: 25 to 31/30, 10: 46/36; of 768, 1: 20/43, 3: 40/48;
+// of 1536, 1: 27 to 30/50, 2: 46/52, 3: 53/52.  The tokens are the capacity of the cache, since the lengths are on the device.
+bool tree_is_small(const elitekv_layer* L, int B, int m, long long max_len) {
+  if ((long long)B * m * L->n_h > 16ll * L->sm_count) return false;
+  const int splits = generic_splits(L, B, m);
+  const long long groups = ((max_len + splits - 1) / splits + kAhead - 1) / kAhead;
+  return groups * (2048 + L->kw + L->vw) <= 12288;
 }
 
 struct GenCarve {
@@ -207,6 +267,6 @@ extern "C" int elitekv_attend_tree(const elitekv_layer* L, const elitekv_cache* 
   if (rc != ELITEKV_OK) return rc;
   if (((uintptr_t)workspace & 255) || workspace_bytes < need) return ELITEKV_ERR_WORKSPACE_TOO_SMALL;
   const TreeCall c{q_rope, q_abs, seq_lens, n_nodes, tree_mask, B, m, workspace, out};
-  return ekv_tree_tc_supported(L, B, m, &cv) ? ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream)
-                                       : ekv_launch_tree_generic(L, cache, cv, c, (cudaStream_t)stream);
+  if (ekv_tree_tc_supported(L, B, m, &cv) && !tree_is_small(L, B, m, cv.max_ctx)) return ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream);
+  return ekv_launch_tree_generic(L, cache, cv, c, (cudaStream_t)stream);
 }
