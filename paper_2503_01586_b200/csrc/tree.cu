@@ -155,6 +155,19 @@ __global__ void tree_generic_kernel(const GenArgs a) {
   }
 }
 
+// How many tokens a single node sees: they are the first ones of its sequence.
+__global__ void tree_single_kernel(const int32_t* seq_lens, const int32_t* n_nodes, const uint64_t* mask, int B, long long max_len, int32_t* lens,
+                                   int32_t* status) {
+  ekv_pdl_wait();
+  ekv_pdl_trigger();
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b >= B) return;
+  const TreeLens t = tree_lens(seq_lens, n_nodes, b, 1, max_len);
+  if (t.bad) ekv_record(status, ELITEKV_ERR_BAD_POSITION, b, seq_lens[b]);
+  lens[b] = t.nodes == 0 ? 0 : t.n - 1 + (int)(mask[b] & 1);
+}
+inline size_t lens_bytes(int B) { return align256(sizeof(int32_t) * (size_t)B); }
+
 // Splits: enough warps for the device
 int generic_splits(const elitekv_layer* L, int B, int m) {
   const long long rows = (long long)B * m * L->n_h, want = 16ll * L->sm_count;
@@ -249,6 +262,8 @@ extern "C" int elitekv_attend_tree_workspace_size(const elitekv_layer* L, int32_
   // the cache's layout is not known here: enough for either kernel
   const size_t g = ekv_tree_generic_bytes(L, B, m), t = ekv_tree_tc_supported(L, B, m, nullptr) ? ekv_tree_tc_bytes(L, B, m) : 0;
   *bytes = g > t ? g : t;
+  size_t d = 0;
+  if (m == 1 && elitekv_decode_workspace_size(L, B, &d) == ELITEKV_OK && d + lens_bytes(B) > *bytes) *bytes = d + lens_bytes(B);
   return ELITEKV_OK;
 }
 
@@ -267,6 +282,14 @@ extern "C" int elitekv_attend_tree(const elitekv_layer* L, const elitekv_cache* 
   if (rc != ELITEKV_OK) return rc;
   if (((uintptr_t)workspace & 255) || workspace_bytes < need) return ELITEKV_ERR_WORKSPACE_TOO_SMALL;
   const TreeCall c{q_rope, q_abs, seq_lens, n_nodes, tree_mask, B, m, workspace, out};
+  if (m == 1) {
+    // One node: decoding over the tokens that it sees, which are the first ones.
+    int32_t* const lens = (int32_t*)workspace;
+    EKV_CUDA_OK(ekv_launch_pdl(tree_single_kernel, dim3((unsigned)((B + 255) / 256)), dim3(256), 0, (cudaStream_t)stream, seq_lens, n_nodes, tree_mask, B,
+                               cv.max_ctx, lens, L->d_status));
+    rc = elitekv_decode(L, cache, q_rope, q_abs, lens, B, (unsigned char*)workspace + lens_bytes(B), workspace_bytes - lens_bytes(B), out, stream);
+    if (rc != ELITEKV_ERR_UNSUPPORTED_SHAPE) return rc;
+  }
   if (ekv_tree_tc_supported(L, B, m, &cv) && !tree_is_small(L, B, m, cv.max_ctx)) return ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream);
   return ekv_launch_tree_generic(L, cache, cv, c, (cudaStream_t)stream);
 }
