@@ -200,7 +200,8 @@ def _layer(case, s, g, max_pos):
     s["elite_dev"] = torch.from_numpy(s["elite"]).to(DEVICE).long()
     if own:
         from paper_2503_01586_b200 import binding as ek
-        W_uk = _normal((kw, n_h * (d_h - 2 * r)), d ** -0.5, g)
+        # no call here reads W_uk: numbers of a generator of its own, so that the inputs are the same either way
+        W_uk = _normal((kw, n_h * (d_h - 2 * r)), d ** -0.5, torch.Generator(device=DEVICE))
         s["layer"] = ek.Layer(n_h, d_h, r, d_c, torch.from_numpy(s["elite"]), W_uk, s["W_uv"], max_pos, cos_sin=s["cos_sin"], d_ck=d_ck)
 
 
