@@ -1,6 +1,7 @@
 // C entry points: argument checks, workspace carving, kernel selection.
 #include "common.cuh"
 #include "plan.cuh"
+#include "tree.cuh"
 
 namespace {
 
@@ -176,7 +177,7 @@ namespace {
 template <class Fn>
 int decode_impl(const elitekv_layer* L, const elitekv_cache* cache, const void* q_rope, const void* q_abs,
                 const int32_t* seq_lens, int32_t B, void* workspace, size_t workspace_bytes, void* out,
-                cudaStream_t st, Fn front, int rows = 1) {
+                cudaStream_t st, Fn front, int rows = 1, const TreeCall* tree = nullptr) {
   if (!L || !cache || !q_abs || !seq_lens || !workspace || !out || B <= 0 || (L->r > 0 && !q_rope))
     return ELITEKV_ERR_INVALID_ARG;
   if (((uintptr_t)q_abs & 15) || ((uintptr_t)out & 3)) return ELITEKV_ERR_INVALID_ARG;
@@ -199,6 +200,8 @@ int decode_impl(const elitekv_layer* L, const elitekv_cache* cache, const void* 
   DecodeScratch ws;
   ws.rows = rows;
   ws.seq_lens = seq_lens;
+  ws.tree_mask = tree ? tree->mask : nullptr;
+  ws.n_nodes = tree ? tree->n_nodes : nullptr;
   ws.max_items = max_items;
   ws.items = (int32_t*)(base + cw.off_items);
   ws.seq_first = (int32_t*)(base + cw.off_first);
@@ -270,4 +273,14 @@ extern "C" int elitekv_attend_rows(const elitekv_layer* L, const elitekv_cache* 
                                    elitekv_stream_t stream) {
   return decode_impl(L, cache, q_rope, q_abs, seq_lens, B, workspace, workspace_bytes, out, (cudaStream_t)stream,
                      [&](const PlanArgs& p, const CacheView&) { return ekv_launch_plan(p, (cudaStream_t)stream); }, m);
+}
+
+size_t ekv_tree_rows_bytes(const elitekv_layer* L, int B, int m) {
+  if (m < 2 || m > ELITEKV_MAX_QUERY_ROWS || (L->decode_kernel != 0 && L->decode_kernel != 2) || !ekv_tc_supported(L, nullptr)) return 0;
+  return carve(L, B, ekv_tc_max_items(L, B, m), m).total;
+}
+
+int ekv_launch_tree_rows(const elitekv_layer* L, const elitekv_cache* cache, const TreeCall& c, size_t workspace_bytes, cudaStream_t st) {
+  return decode_impl(L, cache, c.q_rope, c.q_abs, c.seq_lens, c.B, c.workspace, workspace_bytes, c.out, st,
+                     [&](const PlanArgs& p, const CacheView&) { return ekv_launch_plan(p, st); }, c.m, &c);
 }

@@ -210,6 +210,8 @@ struct DecodeScratch {
   int rows;               // query rows per sequence (1: decode).  With rows > 1 every "n_h" in the shapes
                           // above reads rows * n_h: row i, head h is entry i * n_h + h
   const int32_t* seq_lens;   // rows > 1: the lengths, for the causal limit of each row
+  const uint64_t* tree_mask; // rows are a tree's nodes: [B][rows], the nodes that each sees (null: rows are causal)
+  const int32_t* n_nodes;    // of each sequence's tree (null: rows)
 };
 
 int ekv_combine_fast_ok(const elitekv_layer* L);

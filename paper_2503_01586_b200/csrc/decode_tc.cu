@@ -48,9 +48,14 @@
 //                max / sum in base 2 with a lazily moved reference max, P to shared memory in the
 //                layout the second GEMM wants, TMEM rescale when the reference moves, epilogue
 //                (output blocks transposed through shared memory and written by TMA stores)
+// Tree form (kTree): the query rows are the nodes of a tree of drafted tokens, the sequence's last.  A node sees what
+// is before them and its mask's; the latent rows of the others are cleared before pass B, as the rows behind a
+// sequence's end are, so that nothing of theirs reaches the node.  It serves small calls of elitekv_attend_tree.
+//
 // Every wait is bounded: when a limit is hit the block records ELITEKV_ERR_TIMEOUT in the
 // layer's status word, stops issuing work, frees its TMEM and leaves.
 #include "tc_ptx.cuh"
+#include "tree.cuh"
 
 namespace {
 
@@ -80,6 +85,10 @@ struct TcArgs {
   int rows, gpr, nv;        // query rows per sequence, head groups per row, rows * n_h
   int vparts;               // blocks that share a head group by splitting the OUTPUT columns between them
   const int32_t* seq_lens;  // rows > 1: row i of sequence b sees seq_lens[b] - (rows - 1 - i) tokens
+  const int32_t* n_nodes;   // kTree
+  const uint64_t* mask;
+  int B;
+  long long max_len;
   float scale_log2e;
 };
 
@@ -106,7 +115,7 @@ struct Smem {
   __host__ __device__ static constexpr int total(int d_c) { return misc_off(d_c) + misc_bytes + 1024; }
 };
 
-template <int N, int R2>
+template <int N, int R2, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1)
 decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_constant__ CUtensorMap map_rope,
                  const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_lat128,
@@ -188,6 +197,9 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
   ekv_pdl_wait();
   ekv_pdl_trigger();
   const int item_lo = a.worker_first[worker], item_hi = a.worker_first[worker + 1];
+  if (kTree && blockIdx.x == 0)
+    for (int b = threadIdx.x; b < a.B; b += kThreads)
+      if (tree_lens(a.seq_lens, a.n_nodes, b, a.rows, a.max_len).bad) ekv_record(a.status, ELITEKV_ERR_BAD_POSITION, b, a.seq_lens[b]);
 
   // running counters (each role advances its own copies identically): ring uses, tiles, items
   unsigned lat_n = 0, rope_n = 0, tbase = 0;
@@ -198,9 +210,23 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
   const int tok0 = a.items[4 * item + 1];
   const int ntok = a.items[4 * item + 2];
   const int n_tiles = (ntok + kTile - 1) / kTile;
+  // kTree: tokens before the tree, and the nodes that this block's node sees (asked for by the roles that want them, and
+  // nothing skipped where it sees nothing: a branch around the roles cost the issue of the products its uniform
+  // form, 1.8 us a tile)
+  int prefix = 0;
+  unsigned seen = 0;
+  bool none = false;                   // nothing of the item: its result is zero, whatever the products make of it
+  auto look = [&]() {
+    const TreeLens t = tree_lens(a.seq_lens, a.n_nodes, seq, a.rows, a.max_len);
+    prefix = qrow < t.nodes ? t.n - t.nodes : 0;                     // (a padding node sees nothing)
+    seen = qrow < t.nodes ? (unsigned)a.mask[(size_t)seq * a.rows + qrow] & ((1u << t.nodes) - 1) : 0;
+    none = prefix <= tok0 && (tok0 - prefix >= 32 || (seen >> (tok0 - prefix)) == 0);
+  };
+  auto sees = [&](int t) { return t < prefix || (t - prefix < 32 && (seen >> (t - prefix & 31) & 1) != 0); };       // token of the sequence
   // rotated query chunks of this sequence as fp32 (broadcast operand of the rope dot products):
   // filled and used by the softmax warps only, so nobody else waits for it
   if (warp >= 2 && warp <= 5) {
+    if (kTree) look();
     for (int e = threadIdx.x - 64; e < N * R2; e += kSoftmaxThreads) {
       const int h = e / R2;
       s_qrope[e] = h < nh_here ? __bfloat162float(a.q_rope[((size_t)seq * a.nv + vh0 + h) * R2 + (e % R2)]) : 0.f;
@@ -305,10 +331,15 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
     const uint32_t lo_p = desc_lo(smem_u32(s_p), 128);
     const uint32_t full0 = smem_u32(&bars->lat_full[0]), empty0 = smem_u32(&bars->lat_empty[0]);
     bool ok = true;
+    if (kTree) look();
     for (int tile = 0; tile < n_tiles && ok; ++tile) {
       const int nvalid = min(kTile, ntok - tile * kTile);
       const int ksteps = (nvalid + 15) >> 4;
       const int zero_from = nvalid, zero_to = ksteps * 16;
+      // kTree: the rows to clear, a lane each (at most 15 drafted ones and 15 behind the end, from the first drafted one on)
+      const int t_abs = tok0 + tile * kTile, clear_row = (kTree && !none ? min(max(0, prefix - t_abs), nvalid) : nvalid) + lane;
+      const bool clear = kTree && clear_row < zero_to && (clear_row >= nvalid || !sees(t_abs + clear_row));
+      const bool clear_any = kTree && __any_sync(0xffffffffu, clear);
       const unsigned n0 = lat_n;                 // first ring use of this tile
       // ---- pass A: NKC chunks, 4 K-steps of 16 latent coordinates each
       unsigned slot = n0 % kLatSlots, par = (n0 / kLatSlots) & 1;
@@ -342,7 +373,17 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
         const uint32_t fb = full0 + slot * 8;
         ok = warp_wait(fb, par, s_abort, 5) && warp_wait(fb + 8, par, s_abort, 5);
         if (!ok) break;
-        if (zero_to > zero_from) {
+        if (kTree) {
+          if (clear_any) {
+            if (clear) {       // (the lanes' turns at a row's 16-byte groups keep them on different banks)
+#pragma unroll
+              for (int c16 = 0; c16 < 16; ++c16)
+                *(uint4*)(s_lat + (slot + (c16 >> 3)) * kSlot + clear_row * 128 + ((c16 ^ lane) & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+            __syncwarp();
+          }
+        } else if (zero_to > zero_from) {
           // ragged end of a sequence: rows past its last token inside the last 16-token step are
           // made exact zeros so that zero-probability rows cannot inject NaN/Inf bit patterns
           for (int e = lane; e < (zero_to - zero_from) * 16; e += 32) {
@@ -394,16 +435,17 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
     // lane h holds head h's reference max (N <= 32 per group).  With several query rows a row
     // may see nothing of an item (its causal limit lies before it): a finite start keeps
     // exp2(-inf - m_ref) at zero instead of NaN.
-    float m_ref = a.rows > 1 ? -1e30f : -INFINITY;
+    float m_ref = kTree || a.rows > 1 ? -1e30f : -INFINITY;
     // tokens of this item the block's query row may see (causal rule; all of them when decoding)
     int vis = ntok;
-    if (a.rows > 1) vis = max(0, min(ntok, a.seq_lens[seq] - (a.rows - 1 - qrow) - tok0));
+    if (!kTree && a.rows > 1) vis = max(0, min(ntok, a.seq_lens[seq] - (a.rows - 1 - qrow) - tok0));
     bool ok = true;
     const bool leader = threadIdx.x == 64;
     static_assert(N == 16 || N == 32, "softmax threads keep one head per lane (lanes >= N idle)");
 
     for (int tile = 0; tile < n_tiles && ok; ++tile) {
       const int nvis = min(kTile, vis - tile * kTile);     // rows of the tile this query row sees (may be <= 0)
+      const bool mine = trow < nvis && (!kTree || sees(tok0 + tile * kTile + trow));
       float s[N];
 #pragma unroll
       for (int h = 0; h < N; ++h) s[h] = 0.f;
@@ -452,7 +494,7 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
 #pragma unroll
         for (int h = 0; h < N; ++h) {
           const float x = (s[h] + sv[h]) * a.scale_log2e;
-          s[h] = trow < nvis ? x : -INFINITY;
+          s[h] = mine ? x : -INFINITY;
         }
       }
       // ---- per-head max over the 128 tokens of the tile
@@ -552,7 +594,7 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap map_lat, const __grid_const
         }
         float* tile_s = stage + (size_t)(blk % kOutBufs) * N * 128;
 #pragma unroll
-        for (int h = 0; h < N; ++h) tile_s[h * 128 + trow] = v[h];
+        for (int h = 0; h < N; ++h) tile_s[h * 128 + trow] = none ? 0.f : v[h];
         fence_proxy_async();
         named_bar_sync(1, kSoftmaxThreads);
         if (threadIdx.x == 64) {
@@ -675,6 +717,10 @@ int ekv_launch_decode_tc(const elitekv_layer* L, const elitekv_cache* cache, con
   a.n_groups = a.gpr * rows_q * a.vparts;
   a.nv = rows_q * L->n_h;
   a.seq_lens = ws.seq_lens;
+  a.n_nodes = ws.n_nodes;
+  a.mask = ws.tree_mask;
+  a.B = B;
+  a.max_len = cv.max_ctx;
   a.scale_log2e = L->scale * 1.4426950408889634f;
   const int smem = N == 32 ? Smem<32>::total(L->d_c) : Smem<16>::total(L->d_c);
   auto launch = [&](auto kern) -> int {
@@ -692,16 +738,17 @@ int ekv_launch_decode_tc(const elitekv_layer* L, const elitekv_cache* cache, con
     EKV_CUDA_OK(cudaGetLastError());
     return ELITEKV_OK;
   };
+  const bool tree = ws.tree_mask != nullptr;
   if (N == 32) {
     switch (2 * L->r) {
-      case 8: return launch(decode_tc_kernel<32, 8>);
-      case 16: return launch(decode_tc_kernel<32, 16>);
-      default: return launch(decode_tc_kernel<32, 32>);
+      case 8: return tree ? launch(decode_tc_kernel<32, 8, true>) : launch(decode_tc_kernel<32, 8, false>);
+      case 16: return tree ? launch(decode_tc_kernel<32, 16, true>) : launch(decode_tc_kernel<32, 16, false>);
+      default: return tree ? launch(decode_tc_kernel<32, 32, true>) : launch(decode_tc_kernel<32, 32, false>);
     }
   }
   switch (2 * L->r) {
-    case 8: return launch(decode_tc_kernel<16, 8>);
-    case 16: return launch(decode_tc_kernel<16, 16>);
-    default: return launch(decode_tc_kernel<16, 32>);
+    case 8: return tree ? launch(decode_tc_kernel<16, 8, true>) : launch(decode_tc_kernel<16, 8, false>);
+    case 16: return tree ? launch(decode_tc_kernel<16, 16, true>) : launch(decode_tc_kernel<16, 16, false>);
+    default: return tree ? launch(decode_tc_kernel<16, 32, true>) : launch(decode_tc_kernel<16, 32, false>);
   }
 }

@@ -180,11 +180,28 @@ int generic_splits(const elitekv_layer* L, int B, int m) {
 // tensor-core form hardly depends on so little work (30 to 52 us).  Measured, generic and tensor-core in us, by groups:
 // rows of 64 latents 1: 15/32, 3: 24/32, 5: 25 to 30/32 to 35, 7: 25 to 31/30, 10: 46/36; of 768, 1: 20/43, 3: 40/48;
 // of 1536, 1: 27 to 30/50, 2: 46/52, 3: 53/52.  The tokens are the capacity of the cache, since the lengths are on the device.
-bool tree_is_small(const elitekv_layer* L, int B, int m, long long max_len) {
+// Where nodes can be query rows of the decode kernel (tree_rows_fit; 33, 25 us), a second group is too many.
+bool tree_is_small(const elitekv_layer* L, int B, int m, long long max_len, bool rows_fit) {
   if ((long long)B * m * L->n_h > 16ll * L->sm_count) return false;
   const int splits = generic_splits(L, B, m);
   const long long groups = ((max_len + splits - 1) / splits + kAhead - 1) / kAhead;
-  return groups * (2048 + L->kw + L->vw) <= 12288;
+  return groups * (2048 + L->kw + L->vw) <= (rows_fit ? 6144 : 12288);
+}
+
+// Whether few enough nodes and tokens for the decode kernel, in which every node reads the cache for itself: 20 us less
+// to begin with, and then a time that grows with nodes x tokens and, by 0.3 us, with nodes x sequences.  Measured, that kernel
+// and the tree's own in us, by the sum below in millions: 7B, two nodes over 40 tokens (6) 33/51, 4 x 1000, 4 nodes (66) 45/60,
+// 8 x 2000, 2 (115) 63/78, 4 x 1000, 8 (131) 61/62, 1 x 6000, 8 (155) 61/72, 1 x 3000, 16 (164) 62/59, 2 x 8000, 4 (205)
+// 78/82, 16 x 256, 8 (235) 93/72; 13B, 4 x 1000, 4 (157) 60/69, 1 x 8000, 4 (254) 86/74; 87.5 %, 1 x 6000, 8 (82) 41/78,
+// 32 x 100, 8 (307) 73/69; S-LRD, 32 x 512, 2 (117) 57/70, 1 x 4000, 16 (115) 56/52, 16 x 256, 8 (184) 69/57.
+bool tree_rows_fit(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, int B, int m) {
+  if (ekv_tree_rows_bytes(L, B, m) == 0 || !ekv_tc_supported(L, cache)) return false;
+  long long tokens = cv.max_ctx;
+  if (tokens > 1 << 20 || B > 1 << 10) return false;
+  tokens *= B;
+  if (cv.page_table && ((long long)cv.num_pages << cv.page_shift) < tokens) tokens = (long long)cv.num_pages << cv.page_shift;
+  const int blocks = m * (L->sm_count / ekv_tc_workers(L, 1));          // that read the cache
+  return blocks * (tokens * (L->kw + L->vw) + ((long long)B << 20)) <= 170000000;
 }
 
 struct GenCarve {
@@ -261,7 +278,9 @@ extern "C" int elitekv_attend_tree_workspace_size(const elitekv_layer* L, int32_
   if (!L || !bytes || B <= 0 || m < 1 || m > ELITEKV_MAX_TREE_NODES) return ELITEKV_ERR_INVALID_ARG;
   // the cache's layout is not known here: enough for either kernel
   const size_t g = ekv_tree_generic_bytes(L, B, m), t = ekv_tree_tc_supported(L, B, m, nullptr) ? ekv_tree_tc_bytes(L, B, m) : 0;
+  const size_t r = ekv_tree_rows_bytes(L, B, m);
   *bytes = g > t ? g : t;
+  if (r > *bytes) *bytes = r;
   size_t d = 0;
   if (m == 1 && elitekv_decode_workspace_size(L, B, &d) == ELITEKV_OK && d + lens_bytes(B) > *bytes) *bytes = d + lens_bytes(B);
   return ELITEKV_OK;
@@ -290,6 +309,11 @@ extern "C" int elitekv_attend_tree(const elitekv_layer* L, const elitekv_cache* 
     rc = elitekv_decode(L, cache, q_rope, q_abs, lens, B, (unsigned char*)workspace + lens_bytes(B), workspace_bytes - lens_bytes(B), out, stream);
     if (rc != ELITEKV_ERR_UNSUPPORTED_SHAPE) return rc;
   }
-  if (ekv_tree_tc_supported(L, B, m, &cv) && !tree_is_small(L, B, m, cv.max_ctx)) return ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream);
+  const bool rows_fit = tree_rows_fit(L, cache, cv, B, m), small = tree_is_small(L, B, m, cv.max_ctx, rows_fit);
+  if (rows_fit && !small) {
+    rc = ekv_launch_tree_rows(L, cache, c, workspace_bytes, (cudaStream_t)stream);
+    if (rc != ELITEKV_ERR_UNSUPPORTED_SHAPE) return rc;
+  }
+  if (ekv_tree_tc_supported(L, B, m, &cv) && !small) return ekv_launch_tree_tc(L, cache, cv, c, (cudaStream_t)stream);
   return ekv_launch_tree_generic(L, cache, cv, c, (cudaStream_t)stream);
 }

@@ -35,3 +35,7 @@ int ekv_launch_tree_generic(const elitekv_layer* L, const elitekv_cache* cache, 
 size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m);
 int ekv_tree_tc_supported(const elitekv_layer* L, int B, int m, const CacheView* cv);      // cv may be null: shape alone
 int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const TreeCall& c, cudaStream_t st);
+
+// A node is a query row of the two-pass decode kernel (csrc/decode_tc.cu): small calls of few nodes
+size_t ekv_tree_rows_bytes(const elitekv_layer* L, int B, int m);      // 0: never
+int ekv_launch_tree_rows(const elitekv_layer* L, const elitekv_cache* cache, const TreeCall& c, size_t workspace_bytes, cudaStream_t st);

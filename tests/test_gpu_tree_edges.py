@@ -227,3 +227,40 @@ def test_tables_and_acceptance_on_another_stream_and_captured(ek):
             keep = [x_ for t_, x_ in enumerate(s["where"][b]) if not h <= t_ < h + len(path)]
             assert torch.equal(s["lat"][keep], lat[keep])
     del y
+
+
+# ------------------------------------------------------------------------------- nodes as query rows of the decode kernel
+@pytest.mark.parametrize("ps", [0, 64])
+@pytest.mark.parametrize("w,d_ck", [(gen.LLAMA7B_75, 0), (gen.LLAMA13B_75, 0), (gen.LLAMA7B_75, 512), (gen.SWEEP_875, 0), (layer_of(8, 64, 4, 128), 0),
+                                    (layer_of(24, 64, 16, 256), 128)])
+@pytest.mark.parametrize("m", [2, 7, 15, 16])
+def test_few_nodes_and_tokens(ek, w, d_ck, m, ps):
+    """Trees across the marks of 16 and 128 tokens, with masks that hide any of their nodes, and hidden or padding rows that are
+    not finite."""
+    rng = np.random.default_rng(m + ps)
+    for n in (m, 128, 128 + m // 2, 112 + m, 513):
+        masks = (rng.integers(0, 1 << m, (2, m)) & ~1).astype(np.uint64)       # nobody sees node 0
+        masks[0, m - 1] = 0
+        s = tree_state(ek, w, [n, n - 1], [m, m - 1], m, ps=ps, masks=masks, seed=n, d_ck=d_ck)
+        for b in range(2):
+            s["lat"][s["where"][b][s["lens"][b] - s["nodes"][b]]] = float("nan")
+        check_tree(s, call_tree(ek, s), [0, w.n_h - 1])
+        if n > m:                                                               # what all nodes see, but for the padding one
+            s["rope"][s["where"][1][0]] = s["lat"][s["where"][1][0]] = float("inf")
+            out = call_tree(ek, s)
+            assert not out[1, m - 1].any() and not torch.isfinite(out[1, :m - 1].float()).all(-1).any()
+
+
+@pytest.mark.parametrize("m", [2, 5, 16])
+def test_bad_lengths_of_few_nodes(ek, m):
+    """The same records and rows as in longer calls."""
+    w = gen.LLAMA7B_75
+    s = tree_state(ek, w, [200, 50], [m, m], m, seed=8)
+    good = call_tree(ek, s).clone()
+    for lens, nodes in (([200, 5000], [m, m]), ([200, -3], [m, m]), ([200, 50], [m, m + 1]), ([200, 50], [m, -1]), ([200, 1], [m, m]), ([200, 0], [m, m])):
+        out = ek.elitekv_attend_tree(s["layer"], s["cache"], s["q_rope"], s["q_abs"], i32(lens), i32(nodes), s["mask"], s["ws"])
+        assert ek.elitekv_check_status(s["layer"]) == ek.ERR_BAD_POSITION, (lens, nodes)
+        assert ek.elitekv_last_status_detail(s["layer"])[0] == 1
+        assert torch.equal(out[0], good[0])
+        if lens[1] <= 0 or nodes[1] < 0:
+            assert not out[1].any()
