@@ -58,13 +58,35 @@ constexpr int kOutBytes = 8192;         // rows on their way out, per epilogue w
 enum { kScore = 0, kValue = 1, kStop = 2 };
 
 struct TreeUnit {
-  int type, b, rb, tok0, len, idx, slot, gen, n, nodes, run, k, pad[4];      // 48 bytes are published
+  int kind, b, rb, tok0, len, idx, slot, gen, n, nodes, run, k, pad[4];      // 48 bytes are published; kind: type | layout << 8
+};
+
+// Trees of one call differ in size, and rows of padding nodes cost as much as others.  So row blocks come in layouts: heads of
+// `m` nodes each, `hb` heads a block, `n_rb` row blocks, with n_rb at least a fifth smaller from one to the next.  A sequence
+// has the last that holds its nodes.  (32 ragged sequences of 7B, trees of 7 to 13 nodes: 1035 -> 891 us; 16 of S-LRD, 34 to
+// 64 nodes: 345 -> 316; where all are full, 0.1 to 0.5 us more.)
+constexpr int kLayouts = 8;
+struct TreeLayout {
+  int m, hb, n_rb, n_rc;      // n_rc: 64-column steps that hold the rope columns of any row block
+};
+struct TreeLayouts {
+  int n, tiles;               // tiles: [block][n_rc] of a sequence's spread queries, at most
+  TreeLayout of[kLayouts];
+};
+__device__ __forceinline__ int tree_layout(const TreeLayouts& l, int nodes) {
+  int k = 0;
+  while (k + 1 < l.n && l.of[k + 1].m >= nodes) ++k;
+  return k;
+}
+struct TreeQueryMaps {
+  CUtensorMap of[kLayouts];
 };
 
 struct TreeTcArgs {
   CacheView cv;
   const uint64_t* mask;
-  int m, n_h, r2, kw, vw, hb, n_rb, n_ct, n_rc, box_s, box_v, v3;
+  TreeLayouts lay;
+  int m, n_h, r2, kw, vw, n_rb, n_ct, box_s, box_v, v3;       // n_rb: of the first layout
   float scale_log2e;
   bf16* P;                    // [slot][CG][kPiece / 64][128][64]: what a step loads is one piece (4 KB from row to row: 655 clocks a
                               // step instead of 530)
@@ -75,7 +97,7 @@ struct TreeTcArgs {
   float* part_acc;            // [run][rb][CG][vw / 64][128][64]
   float2* part_ml;            // [run][rb][CG][128]
   const int* hdr;             // [0] claim counter, [1] runs, [2] pieces (row blocks included), [3] D
-  const int4* runs;           // [run][2], by pieces: (b, first token, tokens, pieces), (n, nodes, run, .)
+  const int4* runs;           // [run][2], by pieces: (b, first token, tokens, pieces), (n, nodes, run, layout)
   int32_t* status;
 };
 
@@ -148,7 +170,7 @@ __host__ __device__ __forceinline__ int tree_rope_col(int h0, int r2) { return h
 constexpr int kBins = 256;
 struct PieceWalk {
   int p, at, k, rb;           // piece; run (place in the list), piece of the run, row block
-  int4 r, r2;                 // (b, first token, tokens, pieces), (n, nodes, run, .)
+  int4 r, r2;                 // (b, first token, tokens, pieces), (n, nodes, run, layout)
 };
 __device__ __forceinline__ void walk_load(PieceWalk& w, const TreeTcArgs& a) {
   w.r = a.runs[2 * w.at];
@@ -156,7 +178,7 @@ __device__ __forceinline__ void walk_load(PieceWalk& w, const TreeTcArgs& a) {
 }
 __device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int n_runs, int n_pieces) {
   if (++w.p >= n_pieces) return;
-  if (++w.rb < a.n_rb) return;
+  if (++w.rb < a.lay.of[w.r2.w].n_rb) return;
   w.rb = 0;
   do {
     if (++w.at >= n_runs) { w.at = 0; ++w.k; }
@@ -168,7 +190,7 @@ __device__ __forceinline__ int walk_len(const PieceWalk& w) { return min(kPiece,
 
 template <int CG>
 __global__ void __launch_bounds__(kTreeThreads, 1)
-tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_p,
                const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r,
                const __grid_constant__ CUtensorMap map_ps, const __grid_constant__ CUtensorMap map_o, const TreeTcArgs a) {
@@ -225,7 +247,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   ekv_pdl_trigger();
 
   const int n_blk = (a.vw + 63) >> 6;                         // 64-column blocks of the partial result
-  const int nkl = (a.kw + 63) >> 6, nkc = nkl + a.n_rc;       // steps of a score unit: latents, then rope columns
+  const int nkl = (a.kw + 63) >> 6;                           // steps of a score unit: latents, then rope columns (n_rc)
   // a published unit: what every role waits for, reads and gives back
   unsigned q_pos = 0;
   auto q_slot = [&]() { return q_pos % kQueue; };
@@ -246,16 +268,18 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 1);
       if (!ok) break;
       const volatile TreeUnit* u = s_unit + q_slot();
-      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, n = u->n;
+      const int type = u->kind & 255, lay = u->kind >> 8, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, n = u->n;
       const int prefix = n - u->nodes;
       __syncwarp();
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
         const int all = min(kTile / a.box_s, (n - (tok0 + idx * kTile) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
-        const int h0 = (rb * CG + (int)rank) * a.hb;
-        const uint32_t bytes_b = (uint32_t)(all * a.box_s * 128), bytes_l = (uint32_t)(CG * a.m * a.hb * 128) + bytes_b;
-        const int yq = ((b * a.n_rb + rb) * CG + (int)rank) * a.n_rc * kRows;
+        const TreeLayout& l = a.lay.of[lay];
+        const CUtensorMap* const map_q = &maps_q.of[lay];
+        const int h0 = (rb * CG + (int)rank) * l.hb, nkc = nkl + l.n_rc;
+        const uint32_t bytes_b = (uint32_t)(all * a.box_s * 128), bytes_l = (uint32_t)(CG * l.m * l.hb * 128) + bytes_b;
+        const int yq = (b * a.lay.tiles + (rb * CG + (int)rank) * l.n_rc) * kRows;
         for (int kc = 0; kc < nkc; ++kc, ++pos) {
           const unsigned st = pos % NST;
           ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 2);
@@ -268,7 +292,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           if (elect_one()) {
             if (rank == 0) mbar_expect_tx(fb, lat ? bytes_l : CG * kABytes + bytes_b);
             if (lat) {
-              if (CG == 2) tma_load_4d_pair(dst, &map_q, kc * 64, 0, h0, b, cfb); else tma_load_4d(dst, &map_q, kc * 64, 0, h0, b, cfb);
+              if (CG == 2) tma_load_4d_pair(dst, map_q, kc * 64, 0, h0, b, cfb); else tma_load_4d(dst, map_q, kc * 64, 0, h0, b, cfb);
             } else {
               const int y = yq + (kc - nkl) * kRows;
               if (CG == 2) tma_load_2d_pair(dst, &map_qr, 0, y, cfb); else tma_load_2d(dst, &map_qr, 0, y, cfb);
@@ -312,7 +336,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 17);
       if (!ok) break;
       const volatile TreeUnit* u = s_unit + q_slot();
-      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, n = u->n;
+      const int type = u->kind & 255, lay = u->kind >> 8, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, n = u->n;
       const int prefix = n - u->nodes;
       __syncwarp();
       if (lane == 0) release_unit();
@@ -322,7 +346,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const int bs = a.box_s, mine = min(kTile / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
         int row = 0;
         if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
-        const int xr = tree_rope_col(rb * CG * a.hb, a.r2);
+        const int xr = tree_rope_col(rb * CG * a.lay.of[lay].hb, a.r2), nkc = nkl + a.lay.of[lay].n_rc;
         for (int kc = 0; kc < nkc; ++kc, ++pos) {
           const unsigned st = pos % NST;
           ok = warp_wait(smem_u32(&bars->empty[st]), ((pos / NST) & 1) ^ 1, s_abort, 18);
@@ -396,7 +420,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 5);
         if (!ok) break;
         const volatile TreeUnit* u = s_unit + q_slot();
-        const int type = u->type, tok0 = u->tok0, len = u->len, prefix = u->n - u->nodes;
+        const int type = u->kind & 255, lay = u->kind >> 8, tok0 = u->tok0, len = u->len, prefix = u->n - u->nodes;
         const bool half_tile = a.vw - u->idx * kTile <= kTile / 2;
         __syncwarp();
         if (lane == 0) release_unit();
@@ -406,7 +430,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (!ok) break;
         tc_fence_after();
         const uint32_t d = tmem_base + buf * kTile;
-        const int steps = type == kScore ? nkc : (len + 63) >> 6;
+        const int steps = type == kScore ? nkl + a.lay.of[lay].n_rc : (len + 63) >> 6;
         for (int ks = 0; ks < steps; ++ks, ++pos) {
           const unsigned st = pos % NST;
           ok = warp_wait(smem_u32(&bars->full[st]), (pos / NST) & 1, s_abort, 7);
@@ -446,10 +470,10 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ok = warp_wait_cluster(smem_u32(&bars->q_full[q_slot()]), q_parity(), s_abort, 9);
       if (!ok) break;
       const volatile TreeUnit* u = s_unit + q_slot();
-      const int type = u->type, tok0 = u->tok0, len = u->len, idx = u->idx, n = u->n, prefix = n - u->nodes;
+      const int type = u->kind & 255, lay = u->kind >> 8, tok0 = u->tok0, len = u->len, idx = u->idx, n = u->n, prefix = n - u->nodes;
       if (type == kStop) break;
       if (type == kScore) {
-        pos += nkc;
+        pos += nkl + a.lay.of[lay].n_rc;
       } else {
         const int ks_n = (len + 63) >> 6;
         const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
@@ -551,7 +575,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         // a value unit is published when P of its piece is complete, in both blocks' rows
         if (!stop && !score && !__all_sync(0xffffffffu, lane != 0 || poll_global(a.ready + w.p % kSlots, (w.p / kSlots + 1) * CG, s_abort, 3))) break;
         int x, y, z, t;                        // 16 bytes of the unit per lane
-        if (lane == 0) { x = stop ? kStop : score ? kScore : kValue; y = w.r.x; z = w.rb; t = w.r.y + w.k * kPiece; }
+        if (lane == 0) { x = stop ? kStop : (score ? kScore : kValue) | w.r2.w << 8; y = w.r.x; z = w.rb; t = w.r.y + w.k * kPiece; }
         else if (lane == 1) { x = walk_len(w); y = score ? at : at - n_s; z = w.p % kSlots; t = w.p / kSlots; }
         else { x = w.r2.x; y = w.r2.y; z = w.r2.z; t = w.k; }
         const uint32_t to = smem_u32((const void*)(s_unit + q_slot())) + 16 * lane, bar = smem_u32(&bars->q_full[q_slot()]);
@@ -573,7 +597,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const int group_id = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const bool leader = (threadIdx.x & 127) == 0;
     const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group_id * kTile);
-    const int hl = r / a.m, i = r - hl * a.m;
+    int laid = -1, hl = 0, i = 0;               // the row's head and node in layout `laid`
     volatile int* const verdict = s_verdict + 2 * group_id;
     volatile int* const last = s_last + group_id;
     // rows on their way out: two boxes (128-byte swizzle)
@@ -610,12 +634,17 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     for (q_pos = group_id;; q_pos += 2) {
       if (!group_bar(smem_u32(&bars->q_full[q_slot()]), q_parity(), 12)) break;
       const volatile TreeUnit* u = s_unit + q_slot();
-      const int type = u->type, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, gen = u->gen, n = u->n;
+      const int type = u->kind & 255, lay = u->kind >> 8, b = u->b, rb = u->rb, tok0 = u->tok0, len = u->len, idx = u->idx, slot = u->slot, gen = u->gen, n = u->n;
       const int nodes = u->nodes, run = u->run, k_run = u->k, prefix = n - nodes;
       if (type == kStop) break;
       const uint32_t acc_bar = smem_u32(&bars->acc_full[group_id]), acc_par = (q_pos >> 1) & 1;
-      const int h = (rb * CG + (int)rank) * a.hb + hl;
-      const bool real = hl < a.hb && h < a.n_h, active = real && i < nodes;
+      if (lay != laid) {
+        laid = lay;
+        hl = r / a.lay.of[lay].m;
+        i = r - hl * a.lay.of[lay].m;
+      }
+      const int hb = a.lay.of[lay].hb, h = (rb * CG + (int)rank) * hb + hl;
+      const bool real = hl < hb && h < a.n_h, active = real && i < nodes;
       const unsigned long long mask = active ? a.mask[(long long)b * a.m + i] : 0ull;
       const long long half = (long long)slot * CG + rank;        // this block's share of the slot
       auto acc_done = [&]() {
@@ -845,12 +874,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 struct TreePrepArgs {
   const int32_t *seq_lens, *n_nodes;
   const bf16* q_rope;
-  bf16* qr;                   // [B][row block][block][n_rc][128][64]
-  int B, m, n_rb, n_ct, want, workers, cg, n_h, r2, hb, n_rc, zero_blocks;
+  bf16* qr;                   // [B][lay.tiles: row block, block, n_rc][128][64]
+  TreeLayouts lay;
+  int B, m, n_ct, want, workers, cg, n_h, r2, zero_blocks;
   long long max_len;
   int* hdr;
   int4* runs;
-  int32_t* seq_first;
+  int32_t *seq_first, *seq_lay;
   int* zero;
   int n_zero;
   int32_t* status;
@@ -866,15 +896,18 @@ tree_prep_kernel(const TreePrepArgs a) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (blockIdx.x > a.zero_blocks) {
     // 16 bytes of the spread queries per thread: chunk c's columns [64 c + 8 v, + 8) of a row
-    const long long vecs = (long long)a.B * a.n_rb * a.cg * a.n_rc * kRows * 8;
+    const long long vecs = (long long)a.B * a.lay.tiles * kRows * 8;
     const long long step = (long long)(gridDim.x - 1 - a.zero_blocks) * 256;
     for (long long x = (long long)(blockIdx.x - 1 - a.zero_blocks) * 256 + tid; x < vecs; x += step) {
       const int v = (int)(x & 7), row = (int)(x >> 3) % kRows;
       const long long y = (x >> 3) / kRows;
-      const int c = (int)(y % a.n_rc), block = (int)(y / a.n_rc % (a.n_rb * a.cg)), b = (int)(y / a.n_rc / (a.n_rb * a.cg));
-      const int hl = row / a.m, i = row - hl * a.m, h = block * a.hb + hl;
-      const int col = tree_rope_col(block / a.cg * a.cg * a.hb, a.r2) + c * 64 + v * 8 - h * a.r2;     // of the head's own 2r
-      const bool real = hl < a.hb && h < a.n_h;
+      const int tile = (int)(y % a.lay.tiles), b = (int)(y / a.lay.tiles);
+      const TreeLayout& l = a.lay.of[tree_layout(a.lay, tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len).nodes)];
+      const int c = tile % l.n_rc, block = tile / l.n_rc;
+      if (block >= l.n_rb * a.cg) continue;
+      const int hl = row / l.m, i = row - hl * l.m, h = block * l.hb + hl;
+      const int col = tree_rope_col(block / a.cg * a.cg * l.hb, a.r2) + c * 64 + v * 8 - h * a.r2;     // of the head's own 2r
+      const bool real = hl < l.hb && h < a.n_h;
       const bf16* const q = a.q_rope + (((long long)b * a.m + i) * a.n_h + (real ? h : 0)) * a.r2;
       __align__(16) unsigned short w[8];
 #pragma unroll
@@ -952,7 +985,8 @@ tree_prep_kernel(const TreePrepArgs a) {
       t = tree_lens(a.seq_lens, a.n_nodes, b, a.m, a.max_len);
       cut(t, runs, len, pieces, last);
     }
-    const int items = runs > 0 ? (runs - 1) * pieces + last : 0, scores = runs > 0 ? (t.n + kTile - 1) / kTile : 0;
+    const int lay = tree_layout(a.lay, t.nodes), n_rb = a.lay.of[lay].n_rb;
+    const int items = runs > 0 ? ((runs - 1) * pieces + last) * n_rb : 0, scores = runs > 0 ? (t.n + kTile - 1) / kTile * n_rb : 0;
     int v[3] = {runs, items, scores}, x[3];
 #pragma unroll
     for (int e = 0; e < 3; ++e) {
@@ -974,18 +1008,19 @@ tree_prep_kernel(const TreePrepArgs a) {
     }
     if (b < a.B) {
       a.seq_first[b] = at;
+      a.seq_lay[b] = lay;
       for (int k = 0; k < runs; ++k) {
         const int tok = k * len, l = min(len, t.n - tok), np = k < runs - 1 ? pieces : last;
         const int to = atomicAdd(&s_bin[min(np, kBins)], 1);      // (the order among equals is nobody's concern)
         a.runs[2 * to] = make_int4(b, tok, l, np);
-        a.runs[2 * to + 1] = make_int4(t.n, t.nodes, at + k, 0);
+        a.runs[2 * to + 1] = make_int4(t.n, t.nodes, at + k, lay);
       }
     }
     __syncthreads();
   }
   if (tid == 0) {
     a.seq_first[a.B] = run0;
-    const long long pieces = (long long)item0 * a.n_rb, units = (long long)score0 * a.n_rb + pieces * a.n_ct;
+    const long long pieces = item0, units = score0 + pieces * a.n_ct;
     // how far the score units go ahead of the value units: what the workers hold three and a half times over (1.5 times: 3 to 6 %
     // slower, 2.5: up to 2 %)
     long long d = units > 0 ? (7ll * a.workers * pieces + 2 * units - 1) / (2 * units) : 1;
@@ -1015,9 +1050,10 @@ constexpr int kUpHeld = 8;                // runs whose weights a row keeps
 struct UpArgs {
   const float* part_acc;
   const float2* part_ml;
-  const int32_t* seq_first;
+  const int32_t *seq_first, *seq_lay;
+  TreeLayouts lay;
   bf16* out;
-  int B, m, n_h, d_h, hb, n_half, vw, spt, n_w, n_slots, slot_bytes, group;
+  int B, m, n_h, d_h, n_half, vw, spt, n_w, n_slots, slot_bytes, group;
   int32_t* status;
 };
 template <int N> struct UpRows { static constexpr int value = N; };      // rows of a thread that joins
@@ -1026,7 +1062,7 @@ struct __align__(16) UpBars {
 };
 struct UpSmem {
   static constexpr int a_bytes = 2 * 2 * kRows * 128;                 // 2 stages of head and remainder
-  static constexpr int misc = sizeof(UpBars) + 16 + kRows * (kUpHeld * 4 + 16);
+  static constexpr int misc = sizeof(UpBars) + 16 + kRows * (kUpHeld * 4 + 24);
   __host__ __device__ static constexpr int w_block(int d_h) { return (d_h + 63) / 64 * 8192; }
   __host__ __device__ static constexpr int n_w(int d_h) { return d_h <= 128 ? 3 : 2; }
   __host__ __device__ static constexpr int ring(int d_h) { return d_h <= 128 ? kUpRing : kUpRing - 32 * 1024; }
@@ -1045,8 +1081,9 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   uint32_t* const s_tmem = (uint32_t*)(bars + 1);
   volatile int* const s_abort = (volatile int*)(s_tmem + 1);
   float* const s_wt = (float*)(s_tmem + 4);              // [128][kUpHeld] normalised weights of a row's runs
-  float2* const s_ml = (float2*)(s_wt + kRows * kUpHeld);       // [128] (M, 1 / L)
+  float2* const s_ml = (float2*)(s_wt + kRows * kUpHeld);       // [128] (M, 1 / L); M = -inf: the row sees nothing
   int2* const s_run = (int2*)(s_ml + kRows);             // [128] first run, runs
+  int2* const s_lay = s_run + kRows;                     // [128] the head's first row in a run's partial results, its rows there
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, z = KS > 1 ? (int)cluster_ctarank() : 0;
   const int b0 = blockIdx.x * a.spt, n_seq = min(a.spt, a.B - b0), n_rows = n_seq * a.m;       // this block's sequences and rows
@@ -1091,38 +1128,43 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   ekv_pdl_trigger();
 
   // ---- a row's runs, its largest reference and its sum
-  const int half = h / a.hb, hr = (h - half * a.hb) * a.m;      // the head's rows in a tile of the partial results
   if (tid < kRows) {
-    int2 run = make_int2(0, 0);
+    int2 run = make_int2(0, 0), lay = make_int2(0, 0);
     float M = -1e30f, L = 0.f;
     float2 held[kUpHeld];
 #pragma unroll
     for (int k = 0; k < kUpHeld; ++k) held[k] = make_float2(-1e30f, 0.f);
     const float2* ml = a.part_ml;
     const long long pitch = (long long)a.n_half * kRows;
+    int seen = 0;                          // runs that hold the row: none of a node that its sequence's layout leaves out
     if (tid < n_rows) {
       const int b = b0 + tid / a.m, i = tid % a.m;
       run.x = __ldcg(a.seq_first + b);
       run.y = __ldcg(a.seq_first + b + 1) - run.x;
-      ml += run.x * pitch + half * kRows + hr + i;
+      const TreeLayout& l = a.lay.of[__ldcg(a.seq_lay + b)];
+      const int half = h / l.hb;
+      lay = make_int2(half * kRows + (h - half * l.hb) * l.m, l.m);
+      if (i < l.m) seen = run.y;
+      ml += run.x * pitch + lay.x + i;
 #pragma unroll
       for (int k = 0; k < kUpHeld; ++k)
-        if (k < run.y) held[k] = __ldcg(ml + k * pitch);
+        if (k < seen) held[k] = __ldcg(ml + k * pitch);
 #pragma unroll
       for (int k = 0; k < kUpHeld; ++k) M = fmaxf(M, held[k].x);
-      for (int k = kUpHeld; k < run.y; ++k) M = fmaxf(M, __ldcg(ml + k * pitch).x);
+      for (int k = kUpHeld; k < seen; ++k) M = fmaxf(M, __ldcg(ml + k * pitch).x);
 #pragma unroll
       for (int k = 0; k < kUpHeld; ++k) L = fmaf(held[k].y, exp2f(held[k].x - M), L);
-      for (int k = kUpHeld; k < run.y; ++k) {
+      for (int k = kUpHeld; k < seen; ++k) {
         const float2 x = __ldcg(ml + k * pitch);
         L = fmaf(x.y, exp2f(x.x - M), L);
       }
     }
     const float inv = L != 0.f ? 1.f / L : 0.f;          // (nothing seen: a zero row)
 #pragma unroll
-    for (int k = 0; k < kUpHeld; ++k) s_wt[tid * kUpHeld + k] = k < run.y ? exp2f(held[k].x - M) * inv : 0.f;
-    s_ml[tid] = make_float2(M, inv);
+    for (int k = 0; k < kUpHeld; ++k) s_wt[tid * kUpHeld + k] = k < seen ? exp2f(held[k].x - M) * inv : 0.f;
+    s_ml[tid] = make_float2(L != 0.f ? M : -INFINITY, inv);
     s_run[tid] = run;
+    s_lay[tid] = lay;
   }
   __syncthreads();
   int most = 0;
@@ -1133,14 +1175,15 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
   // normalised weight of a row's k-th run (0: there is none)
   auto weight = [&](int row, int k) -> float {
     if (k < kUpHeld) return s_wt[row * kUpHeld + k];
-    if (k >= s_run[row].y) return 0.f;
-    return exp2f(__ldcg(a.part_ml + ((long long)(s_run[row].x + k) * a.n_half + half) * kRows + hr + row % a.m).x - s_ml[row].x) * s_ml[row].y;
+    if (k >= s_run[row].y || s_ml[row].x == -INFINITY) return 0.f;
+    return exp2f(__ldcg(a.part_ml + (long long)(s_run[row].x + k) * a.n_half * kRows + s_lay[row].x + row % a.m).x - s_ml[row].x) * s_ml[row].y;
   };
 
   if (warp == kUpWarps) {
     // ---- partial results: unit (chunk, `group` runs of every sequence).  A lane copies up to four (run, sequence) pairs.
     const float* src[4];
     int left[4], to[4];                    // runs of the sequence from this one on; place in the unit
+    unsigned bytes[4];
     const int pairs = a.group * n_seq;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -1148,10 +1191,11 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
       const int2 run = x < pairs ? s_run[e * a.m] : make_int2(0, 0);
       left[t] = x < pairs ? run.y - g : 0;
       to[t] = (g * n_rows + e * a.m) * 256;
-      src[t] = a.part_acc + (((long long)run.x + g) * a.n_half + half) * chunks * kRows * 64 + hr * 64;
+      const int2 lay = x < pairs ? s_lay[e * a.m] : make_int2(0, 0);
+      bytes[t] = (unsigned)lay.y * 256;
+      src[t] = a.part_acc + (((long long)run.x + g) * a.n_half + lay.x / kRows) * chunks * kRows * 64 + lay.x % kRows * 64;
     }
     const long long run_pitch = (long long)a.n_half * chunks * kRows * 64;
-    const uint32_t bytes = (uint32_t)a.m * 256;
     int slot = 0;
     uint32_t turn = 1;
     for (int q = 0; q < mine && ok; ++q)
@@ -1159,16 +1203,17 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
         ok = warp_wait(smem_u32(&bars->empty[slot]), turn, s_abort, 1);
         if (!ok) break;
         const int k0 = k * a.group;
-        int n = 0;
+        unsigned n = 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          if (32 * t < pairs) n += __popc(__ballot_sync(0xffffffffu, left[t] > k0));
+          if (left[t] > k0) n += bytes[t];
+        n = __reduce_add_sync(0xffffffffu, n);
         const uint32_t fb = smem_u32(&bars->full[slot]), dst = smem_u32(s_ring) + (uint32_t)slot * a.slot_bytes;
-        if (lane == 0) mbar_expect_tx(fb, (uint32_t)n * bytes);
+        if (lane == 0) mbar_expect_tx(fb, n);
         __syncwarp();
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          if (left[t] > k0) bulk_load(dst + to[t], src[t] + k0 * run_pitch + (long long)(c0 + q) * kRows * 64, bytes, fb);
+          if (left[t] > k0) bulk_load(dst + to[t], src[t] + k0 * run_pitch + (long long)(c0 + q) * kRows * 64, bytes[t], fb);
         __syncwarp();
         if (++slot == a.n_slots) { slot = 0; turn ^= 1; }
       }
@@ -1211,8 +1256,12 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
     auto join = [&](auto rows_per_thread) {
       constexpr int P = decltype(rows_per_thread)::value, U = 4 / P;      // U runs at a time
       int off[P];                          // of a row in a run's share of a unit
+      bool none[P];                        // the row sees nothing (its place may hold anything)
 #pragma unroll
-      for (int p = 0; p < P; ++p) off[p] = min(row_t + kStep * p, n_rows - 1) * 256 + col4 * 16;
+      for (int p = 0; p < P; ++p) {
+        off[p] = min(row_t + kStep * p, n_rows - 1) * 256 + col4 * 16;
+        none[p] = s_ml[row_t + kStep * p].x == -INFINITY;
+      }
       const float* const wt = s_wt + row_t * kUpHeld;
       int slot = 0;
       uint32_t turn = 0;
@@ -1265,7 +1314,7 @@ tree_up_kernel(const __grid_constant__ CUtensorMap map_w, const UpArgs a) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {      // (rows of nobody hold anything)
           const int row = row_t + kStep * p;
-          const float4 v = acc[p];
+          const float4 v = none[p] ? make_float4(0.f, 0.f, 0.f, 0.f) : acc[p];
           const bf162 h0 = __floats2bfloat162_rn(v.x, v.y), h1 = __floats2bfloat162_rn(v.z, v.w);
           const float2 f0 = __bfloat1622float2(h0), f1 = __bfloat1622float2(h1);
           const bf162 l0 = __floats2bfloat162_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2bfloat162_rn(v.z - f1.x, v.w - f1.y);
@@ -1366,21 +1415,31 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // rows of a block are whole heads; one block where it holds all of them, else pairs
 struct TreeShape {
-  int cg, hb, n_rb, n_ct, n_rc, workers, want;
+  int cg, n_rb, n_ct, workers, want;
+  TreeLayouts lay;
 };
 TreeShape tree_shape(const elitekv_layer* L, int m) {
   TreeShape s;
   const int most = kRows / m, blocks = (L->n_h + most - 1) / most;
   s.cg = blocks == 1 ? 1 : 2;
   s.n_rb = (blocks + s.cg - 1) / s.cg;
-  s.hb = (L->n_h + s.n_rb * s.cg - 1) / (s.n_rb * s.cg);
-  s.n_ct = (L->vw + kTile - 1) / kTile;
-  s.n_rc = 0;                              // 64-column steps that hold the rope columns of any row block
-  for (int rb = 0; rb < s.n_rb && L->r > 0; ++rb) {
-    const int h0 = rb * s.cg * s.hb, h1 = h0 + s.cg * s.hb < L->n_h ? h0 + s.cg * s.hb : L->n_h;
-    const int steps = h1 > h0 ? (h1 * 2 * L->r - tree_rope_col(h0, 2 * L->r) + 63) / 64 : 0;
-    s.n_rc = steps > s.n_rc ? steps : s.n_rc;
+  s.lay.n = s.lay.tiles = 0;
+  for (int k = m; k >= 1 && s.lay.n < kLayouts; --k) {
+    const int n = (L->n_h + kRows / k - 1) / (kRows / k), n_rb = (n + s.cg - 1) / s.cg;
+    if (s.lay.n > 0 && n_rb * 5 > s.lay.of[s.lay.n - 1].n_rb * 4) continue;
+    TreeLayout& l = s.lay.of[s.lay.n++];
+    l.m = k;
+    l.n_rb = n_rb;
+    l.hb = (L->n_h + n_rb * s.cg - 1) / (n_rb * s.cg);
+    l.n_rc = 0;
+    for (int rb = 0; rb < n_rb && L->r > 0; ++rb) {
+      const int h0 = rb * s.cg * l.hb, h1 = h0 + s.cg * l.hb < L->n_h ? h0 + s.cg * l.hb : L->n_h;
+      const int steps = h1 > h0 ? (h1 * 2 * L->r - tree_rope_col(h0, 2 * L->r) + 63) / 64 : 0;
+      l.n_rc = steps > l.n_rc ? steps : l.n_rc;
+    }
+    if (n_rb * s.cg * l.n_rc > s.lay.tiles) s.lay.tiles = n_rb * s.cg * l.n_rc;
   }
+  s.n_ct = (L->vw + kTile - 1) / kTile;
   s.workers = L->sm_count / s.cg;
   s.want = s.workers / (s.n_rb * s.n_ct);
   if (s.want < 1) s.want = 1;
@@ -1388,7 +1447,7 @@ TreeShape tree_shape(const elitekv_layer* L, int m) {
 }
 
 struct TreeCarve {
-  size_t hdr, runs, first, zero, n_zero, stats, pref, cstate, P, qr, ml, acc, total;
+  size_t hdr, runs, first, lay, zero, n_zero, stats, pref, cstate, P, qr, ml, acc, total;
   size_t max_runs;
 };
 TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
@@ -1399,13 +1458,14 @@ TreeCarve tree_carve(const elitekv_layer* L, const TreeShape& s, int B, int m) {
   c.hdr = o;    o = align256(o + 16);
   c.runs = o;   o = align256(o + c.max_runs * 32);
   c.first = o;  o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
+  c.lay = o;    o = align256(o + sizeof(int32_t) * (size_t)B);
   c.n_zero = (size_t)kSlots * (s.cg + 2) + chains;
   c.zero = o;   o = align256(o + sizeof(int) * c.n_zero);
   c.stats = o;  o = align256(o + sizeof(float2) * kSlots * s.cg * kTiles * kRows);
   c.pref = o;   o = align256(o + sizeof(float2) * kSlots * s.cg * kRows);
   c.cstate = o; o = align256(o + sizeof(float2) * chains * s.cg * kRows);
   c.P = o;      o = align256(o + sizeof(bf16) * (size_t)kSlots * s.cg * kRows * kPiece);
-  c.qr = o;     o = align256(o + sizeof(bf16) * (size_t)B * s.n_rb * s.cg * s.n_rc * kRows * 64);
+  c.qr = o;     o = align256(o + sizeof(bf16) * (size_t)B * s.lay.tiles * kRows * 64);
   const size_t tile_rows = c.max_runs * s.n_rb * s.cg * kRows;
   c.ml = o;     o = align256(o + sizeof(float2) * tile_rows);
   c.acc = o;    o = align256(o + sizeof(float) * tile_rows * ((L->vw + 63) / 64) * 64);
@@ -1443,13 +1503,13 @@ int make_map_chunks(CUtensorMap* m, const void* ptr, unsigned long long rows, un
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
 }
-// queries [B][m][n_h][kw] seen as (sequence, head, node, latent): a box is `hb` heads of m nodes each
-int make_map_queries(CUtensorMap* map, const void* ptr, int B, int m, int n_h, int kw, int hb) {
+// queries [B][m][n_h][kw] seen as (sequence, head, node, latent): a box is `hb` heads, the first `nodes` nodes of each
+int make_map_queries(CUtensorMap* map, const void* ptr, int B, int m, int n_h, int kw, int hb, int nodes) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return ELITEKV_ERR_CUDA;
   cuuint64_t dims[4] = {(cuuint64_t)kw, (cuuint64_t)m, (cuuint64_t)n_h, (cuuint64_t)B};
   cuuint64_t strides[3] = {(cuuint64_t)n_h * kw * 2, (cuuint64_t)kw * 2, (cuuint64_t)m * n_h * kw * 2};
-  cuuint32_t box[4] = {64, (cuuint32_t)m, (cuuint32_t)hb, 1}, estr[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {64, (cuuint32_t)nodes, (cuuint32_t)hb, 1}, estr[4] = {1, 1, 1, 1};
   CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ELITEKV_OK : ELITEKV_ERR_CUDA;
@@ -1468,7 +1528,7 @@ size_t ekv_tree_tc_bytes(const elitekv_layer* L, int B, int m) { return tree_car
 int ekv_tree_tc_supported(const elitekv_layer* L, int B, int m, const CacheView* cv) {
   const TreeShape s = tree_shape(L, m);
   if (((unsigned long long)B + s.want) * s.n_rb * s.cg * ((L->vw + 63) / 64) * kRows >= (1ull << 31) ||
-      (unsigned long long)B * s.n_rb * s.cg * s.n_rc * kRows >= (1ull << 31) || L->n_h > 65535)
+      (unsigned long long)B * s.lay.tiles * kRows >= (1ull << 31) || L->n_h > 65535)
     return 0;
   if ((L->n_h * L->r) % 4 != 0) return 0;
   if (L->d_h % 16 != 0 || L->d_h > 256) return 0;          // the last product's width
@@ -1479,8 +1539,9 @@ int ekv_tree_tc_supported(const elitekv_layer* L, int B, int m, const CacheView*
 }
 
 int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const CacheView& cv, const TreeCall& c, cudaStream_t st) {
-  const TreeShape s = tree_shape(L, c.m);
+  TreeShape s = tree_shape(L, c.m);
   const TreeCarve w = tree_carve(L, s, c.B, c.m);
+  if (c.n_nodes == nullptr) s.lay.n = 1;
   unsigned char* const base = (unsigned char*)c.workspace;
   const int page = cv.page_table ? 1 << cv.page_shift : 1 << 30;
   TreeTcArgs a;
@@ -1491,10 +1552,9 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.r2 = 2 * L->r;
   a.kw = L->kw;
   a.vw = L->vw;
-  a.hb = s.hb;
+  a.lay = s.lay;
   a.n_rb = s.n_rb;
   a.n_ct = s.n_ct;
-  a.n_rc = s.n_rc;
   a.box_s = page < 128 ? page : 128;
   a.box_v = page < 64 ? page : 64;
   a.scale_log2e = L->scale * 1.4426950408889634f;
@@ -1511,12 +1571,17 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   a.hdr = (const int*)(base + w.hdr);
   a.runs = (const int4*)(base + w.runs);
   a.status = L->d_status;
-  CUtensorMap m_q, m_k, m_v, m_p, m_qr, m_r, m_ps, m_o, m_w;
+  TreeQueryMaps m_q;
+  CUtensorMap m_k, m_v, m_p, m_qr, m_r, m_ps, m_o, m_w;
   a.v3 = a.box_v == 64 && L->vw % 64 == 0;
   const unsigned long long p_rows = (unsigned long long)kSlots * s.cg * (kPiece / 64) * kRows;
   const unsigned long long blk_rows = (unsigned long long)w.max_runs * s.n_rb * s.cg * ((L->vw + 63) / 64) * kRows;
   const unsigned long long rows = plane_rows(cv);
-  int rc = make_map_queries(&m_q, c.q_abs, c.B, c.m, L->n_h, L->kw, s.hb);
+  int rc = ELITEKV_OK;
+  for (int k = 0; k < kLayouts && rc == ELITEKV_OK; ++k) {
+    if (k < s.lay.n) rc = make_map_queries(&m_q.of[k], c.q_abs, c.B, c.m, L->n_h, L->kw, s.lay.of[k].hb, s.lay.of[k].m);
+    else m_q.of[k] = m_q.of[0];
+  }
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_k, cache->latent, rows, L->kw, L->d_c, a.box_s);
   if (rc == ELITEKV_OK)
     rc = a.v3 ? make_map_chunks(&m_v, (const bf16*)cache->latent + L->voff, rows, L->vw, L->d_c, 4 / s.cg)
@@ -1527,8 +1592,8 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   if (rc == ELITEKV_OK) rc = make_map_pitch(&m_p, a.P, p_rows, 64, 64, kRows);
   // (a layer without rope has neither; the maps are not used)
   m_qr = m_r = m_p;
-  if (rc == ELITEKV_OK && s.n_rc > 0) {
-    rc = make_map_pitch(&m_qr, base + w.qr, (unsigned long long)c.B * s.n_rb * s.cg * s.n_rc * kRows, 64, 64, kRows);
+  if (rc == ELITEKV_OK && s.lay.tiles > 0) {
+    rc = make_map_pitch(&m_qr, base + w.qr, (unsigned long long)c.B * s.lay.tiles * kRows, 64, 64, kRows);
     if (rc == ELITEKV_OK) rc = make_map_pitch(&m_r, cache->rope, rows, (unsigned long long)L->n_h * a.r2, (unsigned long long)L->n_h * a.r2, a.box_s);
   }
   if (rc != ELITEKV_OK) return rc;
@@ -1538,13 +1603,11 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   p.cg = s.cg;
   p.n_h = L->n_h;
   p.r2 = a.r2;
-  p.hb = s.hb;
-  p.n_rc = s.n_rc;
+  p.lay = s.lay;
   p.seq_lens = c.seq_lens;
   p.n_nodes = c.n_nodes;
   p.B = c.B;
   p.m = c.m;
-  p.n_rb = s.n_rb;
   p.n_ct = s.n_ct;
   p.want = s.want;
   p.workers = s.workers;
@@ -1552,12 +1615,13 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   p.hdr = (int*)(base + w.hdr);
   p.runs = (int4*)(base + w.runs);
   p.seq_first = (int32_t*)(base + w.first);
+  p.seq_lay = (int32_t*)(base + w.lay);
   p.zero = a.s_cnt;
   p.n_zero = (int)w.n_zero;
   p.status = L->d_status;
   const int zero_blocks = (p.n_zero + 1023) / 1024;
   p.zero_blocks = zero_blocks < 32 ? zero_blocks : 32;
-  const long long qr_blocks = ((long long)c.B * s.n_rb * s.cg * s.n_rc * kRows * 8 + 1023) / 1024;
+  const long long qr_blocks = ((long long)c.B * s.lay.tiles * kRows * 8 + 1023) / 1024;
   EKV_CUDA_OK(ekv_launch_pdl(tree_prep_kernel, dim3((unsigned)(1 + p.zero_blocks + (qr_blocks < 1024 ? qr_blocks : 1024))), dim3(256), 0, st, p));
   const int smem = s.cg == 2 ? TreeSmem<2>::total : TreeSmem<1>::total;
   auto launch = [&](auto kern) -> int {
@@ -1591,7 +1655,8 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   u.m = c.m;
   u.n_h = L->n_h;
   u.d_h = L->d_h;
-  u.hb = s.hb;
+  u.seq_lay = p.seq_lay;
+  u.lay = s.lay;
   u.n_half = s.n_rb * s.cg;
   u.vw = L->vw;
   u.status = L->d_status;

@@ -264,3 +264,23 @@ def test_bad_lengths_of_few_nodes(ek, m):
         assert torch.equal(out[0], good[0])
         if lens[1] <= 0 or nodes[1] < 0:
             assert not out[1].any()
+
+
+# ------------------------------------------------------------------------------- trees of one call that differ in size
+@pytest.mark.parametrize("w,d_ck,m", [(gen.LLAMA7B_75, 0, 64), (gen.LLAMA7B_75, 0, 21), (gen.LLAMA7B_75, 512, 64), (gen.LLAMA13B_75, 0, 33),
+                                      (gen.SWEEP_875, 0, 50), (layer_of(12, 64, 4, 200), 0, 64), (layer_of(80, 32, 2, 64), 0, 64),
+                                      (layer_of(20, 48, 0, 72), 0, 64), (layer_of(6, 256, 2, 136), 8, 64)])
+def test_ragged_trees(ek, w, d_ck, m):
+    """Every number of nodes from none to m in one call, in runs of several pieces and in short ones; the rows behind a
+    sequence's nodes are zero, whatever their queries hold, and a sequence's result is that of a call of its own."""
+    rng = np.random.default_rng(m)
+    nodes = [m, 0] + sorted(rng.permutation(np.arange(1, m))[:14].tolist()) + [1, m // 2, m // 2 + 1, m // 4, m - 1]
+    lens = [int(k + rng.integers(0, 700)) if k % 3 else k + (2600 if k in (m, 1) else 0) for k in nodes]
+    s = tree_state(ek, w, lens, nodes, m, ps=32, seed=m, d_ck=d_ck)
+    for b, k in enumerate(nodes):
+        s["q_abs"][b, k:] = float("nan")
+        s["q_rope"][b, k:] = float("inf")
+    out = call_tree(ek, s)
+    check_tree(s, out, [0, w.n_h - 1])
+    again = call_tree(ek, s)
+    assert torch.equal(out, again)
