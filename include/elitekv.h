@@ -271,8 +271,8 @@ int elitekv_step_tables(const elitekv_cache* cache, const elitekv_tables* tables
                         int64_t n_slots, elitekv_stream_t stream);
 
 /* elitekv_append with the cache row of every token given (elitekv_step_tables) instead of its
- * sequence: token t is rotated at pos[t] and written to row slot[t] of the planes; a negative slot is
- * padding and writes nothing.  A slot outside the planes or a position outside [0, max_pos) is
+ * sequence: token t is rotated at pos[t] and written to row slot[t] of the planes (no slot twice); a
+ * negative slot is padding and writes nothing.  A slot outside the planes or a position outside [0, max_pos) is
  * recorded (BAD_POSITION, detail = token, position) and skipped. */
 int elitekv_append_slots(const elitekv_layer* layer, const elitekv_cache* cache, const void* k_e, const void* c,
                          const int64_t* slot, const int32_t* pos, int64_t T, elitekv_stream_t stream);
@@ -289,7 +289,9 @@ int elitekv_append_slots(const elitekv_layer* layer, const elitekv_cache* cache,
  *   tree_mask uint64 [B][m];   out bf16 [B][m][n_h][d_h], 4-byte aligned
  *   workspace: 256-byte aligned, elitekv_attend_tree_workspace_size bytes (of shape, B, m and device, not
  *   of the lengths), private to this call until the stream reaches its end.
- * 1 <= m <= ELITEKV_MAX_TREE_NODES; any layer and page size.  Results do not depend on scheduling. */
+ * 1 <= m <= ELITEKV_MAX_TREE_NODES; any layer and page size.  Results do not depend on scheduling.
+ * A length outside the cache and a node count outside [0, m] or above the length are recorded (BAD_POSITION,
+ * detail = sequence, length) and clamped, a page id outside the pool (BAD_PAGE) counts as page 0. */
 int elitekv_attend_tree_workspace_size(const elitekv_layer* layer, int32_t B, int32_t m, size_t* bytes);
 int elitekv_attend_tree(const elitekv_layer* layer, const elitekv_cache* cache, const void* q_rope, const void* q_abs,
                         const int32_t* seq_lens, const int32_t* n_nodes, const uint64_t* tree_mask, int32_t B, int32_t m,

@@ -86,7 +86,7 @@ step_tables_kernel(const TabArgs a) {
     long long nt = 0, np = 0;
     if (b < a.B) {
       const long long held = t.held[b], fresh = t.fresh[b];
-      const bool bad = held < 0 || fresh < 0 || held + fresh > max_len || (a.m > 0 && fresh > a.m);
+      const bool bad = held < 0 || fresh < 0 || held + fresh > max_len || held + fresh > 0x7fffffffll || (a.m > 0 && fresh > a.m);
       const long long ph = paged ? t.pages_held[b] : 0;
       if (bad || (paged && (ph < (held + a.cv.page_mask) >> shift || ph > a.cv.max_pages_per_seq))) {
         atomicMin(&s_bad, b);

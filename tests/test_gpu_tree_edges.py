@@ -284,3 +284,14 @@ def test_ragged_trees(ek, w, d_ck, m):
     check_tree(s, out, [0, w.n_h - 1])
     again = call_tree(ek, s)
     assert torch.equal(out, again)
+
+
+def test_tables_of_lengths_that_pass_31_bits(ek):
+    """A page table wide enough for 2^32 tokens, a sequence whose new length is no int32: refused before its pages are read."""
+    table = i32(np.full((1, 8), -1))
+    plane = torch.zeros(8, dtype=torch.bfloat16, device="cuda")
+    cache = ek.make_cache(plane, plane, n_seqs=1, page_table=table, page_size=128)
+    cache.max_pages_per_seq, cache.num_pages = 1 << 25, 1 << 25
+    t = ek.make_tables(1, 16, 0, i32([(1 << 31) - 3]), i32([5]), page_table=table, pages_held=i32([1 << 24]), free_pages=i32([0]), n_free=i32([0]))
+    ek.elitekv_step_tables(cache, t)
+    assert t.result.tolist() == [ek.ERR_BAD_POSITION, 0, 0, 0] and t.slot.tolist() == [-1] * 16 and t.seq_lens.tolist() == [(1 << 31) - 3]
