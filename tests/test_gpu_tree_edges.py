@@ -295,3 +295,11 @@ def test_tables_of_lengths_that_pass_31_bits(ek):
     t = ek.make_tables(1, 16, 0, i32([(1 << 31) - 3]), i32([5]), page_table=table, pages_held=i32([1 << 24]), free_pages=i32([0]), n_free=i32([0]))
     ek.elitekv_step_tables(cache, t)
     assert t.result.tolist() == [ek.ERR_BAD_POSITION, 0, 0, 0] and t.slot.tolist() == [-1] * 16 and t.seq_lens.tolist() == [(1 << 31) - 3]
+
+
+@pytest.mark.parametrize("w,d_ck", [(gen.LLAMA7B_75, 0), (gen.LLAMA13B_75, 0), (gen.LLAMA7B_75, 512), (gen.TINY, 0)])
+@pytest.mark.parametrize("ps", [4, 8, 32])
+def test_one_node_over_small_pages(ek, w, d_ck, ps):
+    """Pages that no decode kernel on the tensor cores takes."""
+    s = tree_state(ek, w, [3000, 1, 700], [1, 1, 0], 1, ps=ps, masks=np.array([[1], [1], [1]], dtype=np.uint64), seed=ps, d_ck=d_ck)
+    check_tree(s, call_tree(ek, s), [0, w.n_h - 1])
