@@ -341,9 +341,11 @@ def elitekv_step_tables(cache: CacheDesc, tables: Tables) -> Tables:
 
 def elitekv_append_slots(layer: Layer, cache: CacheDesc, k_e, c, slot, pos) -> None:
     """slot int64 [T] (rows of the planes, negative: padding), pos int32 [T]."""
-    bf16 = torch.bfloat16
-    _check(lib().elitekv_append_slots(layer.handle, C.byref(cache), _ptr(k_e), _in(c, bf16), _in(slot, torch.int64),
-                                      _in(pos, torch.int32), c.shape[0], _stream()), "elitekv_append_slots")
+    bf16, T = torch.bfloat16, c.shape[0]
+    if slot.numel() < T or pos.numel() < T or c.numel() != T * layer.d_c or (layer.r and k_e.numel() != T * layer.n_h * layer.r * 2):
+        raise ValueError("elitekv_append_slots: k_e [T][n_h][r][2], c [T][d_c], slot [T], pos [T]")
+    _check(lib().elitekv_append_slots(layer.handle, C.byref(cache), None if k_e is None else _in(k_e, bf16), _in(c, bf16),
+                                      _in(slot, torch.int64), _in(pos, torch.int32), T, _stream()), "elitekv_append_slots")
 
 
 def elitekv_attend_tree_workspace_size(layer: Layer, B: int, m: int) -> int:
@@ -357,11 +359,16 @@ def elitekv_attend_tree(layer: Layer, cache: CacheDesc, q_rope, q_abs, seq_lens,
     the node sees node j) -> out [B][m][n_h][d_h]."""
     B, m = tree_mask.shape
     bf16, i32 = torch.bfloat16, torch.int32
-    if q_abs.numel() != B * m * layer.n_h * layer.kw:
-        raise ValueError("elitekv_attend_tree: q_abs is [B][m][n_h][kw]")
+    rows = B * m * layer.n_h
+    if q_abs.numel() != rows * layer.kw or (layer.r and q_rope.numel() != rows * 2 * layer.r):
+        raise ValueError("elitekv_attend_tree: q_abs is [B][m][n_h][kw], q_rope [B][m][n_h][2r]")
+    if seq_lens.numel() < B or (n_nodes is not None and n_nodes.numel() < B):
+        raise ValueError("elitekv_attend_tree: seq_lens and n_nodes have an entry per sequence")
     if out is None:
         out = torch.empty((B, m, layer.n_h, layer.d_h), dtype=bf16, device=q_abs.device)
-    _check(lib().elitekv_attend_tree(layer.handle, C.byref(cache), _ptr(q_rope), _in(q_abs, bf16), _in(seq_lens, i32),
+    elif out.numel() != rows * layer.d_h:
+        raise ValueError("elitekv_attend_tree: out is [B][m][n_h][d_h]")
+    _check(lib().elitekv_attend_tree(layer.handle, C.byref(cache), None if q_rope is None else _in(q_rope, bf16), _in(q_abs, bf16), _in(seq_lens, i32),
                                      None if n_nodes is None else _in(n_nodes, i32), _in(tree_mask, torch.int64), B, m,
                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _in(out, bf16), _stream()),
            "elitekv_attend_tree")
@@ -373,7 +380,12 @@ def elitekv_accept_tree(layer: Layer, cache: CacheDesc, held, n_nodes, parent, d
     """held, n_nodes (None: m), first int32 [B], parent (None: chain), draft, chosen int32 [B][m].
     Returns (n_accepted [B], path [B][m], token [B], held_out [B])."""
     B, m = draft.shape
-    i32 = torch.int32
+    i32, nodes = torch.int32, draft.numel()
+    if chosen.numel() != nodes or (parent is not None and parent.numel() != nodes) or (path is not None and path.numel() != nodes):
+        raise ValueError("elitekv_accept_tree: draft, chosen, parent and path are [B][m]")
+    for v in (held, first, n_nodes, n_accepted, token, held_out):
+        if v is not None and v.numel() < B:
+            raise ValueError("elitekv_accept_tree: held, first, n_nodes, n_accepted, token and held_out have an entry per sequence")
     if n_accepted is None:
         n_accepted = torch.empty(B, dtype=i32, device=draft.device)
     if path is None:
