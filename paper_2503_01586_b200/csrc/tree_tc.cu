@@ -22,7 +22,7 @@
 // go on, whatever else runs on the device.
 //
 // Softmax reference.  P is bf16 and O fp32: both have 8 exponent bits, so the reference of 2^(S - ref) only has to keep
-// the exponents in range.  It is 0 while the largest score of (row, 128 tokens) is within 2^+-64, else a multiple of
+// the exponents in range.  It is 0 while the largest score of (row, 256 tokens) is within 2^+-64, else a multiple of
 // 64 near it.  All tiles of a row agree on it unless scores are extreme; the block that finishes a piece's last
 // score unit looks, and brings P of rows that do not agree to the largest reference: a factor of a power of two, exact.
 // The sums are of the rounded P, so that their rounding cancels where one token dominates.
