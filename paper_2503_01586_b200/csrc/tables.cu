@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(kTabThreads)
 step_tables_kernel(const TabArgs a) {
   extern __shared__ int s_tab[];               // first token [B+1], first new page [B+1]
   __shared__ long long s_sum[2][kTabWarps];
-  __shared__ int s_bad, s_page;
+  __shared__ int s_bad;
+  __shared__ long long s_page;                  // a bad page id among those that new tokens go to: any int32 may be one
   int* const s_tok = s_tab;
   int* const s_pg = s_tab + a.B + 1;
   const elitekv_tables& t = a.t;
@@ -73,8 +74,12 @@ step_tables_kernel(const TabArgs a) {
   const bool paged = a.cv.page_table != nullptr;
   const int shift = a.cv.page_shift;
   const long long max_len = paged ? (long long)a.cv.max_pages_per_seq << shift : a.cv.max_ctx;
-  constexpr int kNone = 0x7fffffff;
-  if (tid == 0) s_bad = s_page = kNone;
+  constexpr int kNone = 0x7fffffff;             // no sequence
+  constexpr long long kNoPage = 1ll << 32;
+  if (tid == 0) {
+    s_bad = kNone;
+    s_page = kNoPage;
+  }
   ekv_pdl_wait();
   ekv_pdl_trigger();
   __syncthreads();
@@ -98,7 +103,7 @@ step_tables_kernel(const TabArgs a) {
           // pages of the sequence's own that new tokens go to
           for (long long p = held >> shift; p < (end < ph ? end : ph) && fresh > 0; ++p) {
             const int id = t.page_table[(long long)b * a.cv.max_pages_per_seq + p];
-            if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, id < 0 ? -1 : id);
+            if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, (long long)(id < 0 ? -1 : id));
           }
         }
       }
@@ -141,13 +146,13 @@ step_tables_kernel(const TabArgs a) {
   } else {
     for (int k = tid; k < (int)pg0; k += kTabThreads) {
       const int id = t.free_pages[n_free - 1 - k];
-      if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, id < 0 ? -1 : id);
+      if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, (long long)(id < 0 ? -1 : id));
     }
   }
   __syncthreads();
-  if (status == ELITEKV_OK && s_page != kNone) {
+  if (status == ELITEKV_OK && s_page != kNoPage) {
     status = ELITEKV_ERR_BAD_PAGE;
-    detail = s_page;
+    detail = (int)s_page;
   }
   const bool ok = status == ELITEKV_OK;
 
