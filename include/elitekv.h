@@ -221,6 +221,8 @@ int elitekv_attend_rows(const elitekv_layer* layer, const elitekv_cache* cache, 
  *   elitekv_absorb_query  on the B*m rows, q_pos = pos
  *   elitekv_attend_tree   attention of every node over the committed tokens and its ancestors
  *   elitekv_accept_tree   the branch that the model confirms joins the committed tokens
+ * The last two take the tables' `granted` as n_nodes, not `fresh`: a refused step has cached no drafts, and with 0
+ * nodes its rows are zero and held and first stay, also where no host looks at the status (a captured step).
  * Node i of sequence b is cached at position held[b] + i; its parent is a node before it, or -1 for
  * the committed tokens (an entry that is not a node before i counts as -1).  The paper has no
  * counterpart of the tables and the acceptance; the attention is the score equation of Section 3.1
@@ -250,6 +252,8 @@ typedef struct {
   int64_t* slot;               /* [n_slots] cache row, -1 in padding                                  */
   uint64_t* tree_mask;         /* [B][m] (m > 0): bit j = node i sees node j; 0 in padding            */
   int32_t* result;             /* [4]: status, new tokens, pages taken, detail                        */
+  int32_t* granted;            /* [B], or NULL: new tokens of the sequence that the step holds: fresh,
+                                  or 0 in a refused step.  The node count of the calls that follow    */
 } elitekv_tables;
 
 /* Page table, slot map, rotary positions and tree masks of a step from the request lengths, on the
@@ -265,7 +269,7 @@ typedef struct {
  *                             than m, fewer pages held than tokens; or -1: more tokens than n_slots
  *   ELITEKV_ERR_BAD_PAGE      result[3]: a page id outside the pool, among those the new tokens go to
  * and then nothing is granted: the page table is as it was, every entry is padding, seq_lens = held,
- * first = 0, pages_held_out = pages_held, n_free_out = n_free.
+ * first = 0, granted = 0, pages_held_out = pages_held, n_free_out = n_free.
  * B <= ELITEKV_MAX_TABLE_SEQS, sequences 0 .. B-1 of the cache. */
 int elitekv_step_tables(const elitekv_cache* cache, const elitekv_tables* tables, int32_t B, int32_t m,
                         int64_t n_slots, elitekv_stream_t stream);
@@ -301,7 +305,8 @@ int elitekv_attend_tree(const elitekv_layer* layer, const elitekv_cache* cache, 
  * after node i.  The accepted branch starts at the lowest node on the committed tokens that drafts first[b]; a node
  * is followed by its lowest child that drafts what was chosen after it.  Its k-th node's cache row moves, bit for
  * bit, to position held[b] + k (the position it was rotated at).
- *   held int32 [B] committed tokens, n_nodes int32 [B] (NULL: m), parent (NULL: a chain), draft, chosen int32 [B][m]
+ *   held int32 [B] committed tokens, n_nodes int32 [B] cached nodes (NULL: m; clamped to [0, m]), parent (NULL: a
+ *   chain), draft, chosen int32 [B][m]
  *   n_accepted int32 [B]; path int32 [B][m]: the branch, then -1; token int32 [B]: the choice after the branch (the
  *   next step's `first`); held_out int32 [B] = held + n_accepted.  held_out may be held, token may be first.
  * Pages beyond the accepted tokens stay with their sequence (elitekv_step_tables uses them first).  A page id outside

@@ -53,7 +53,7 @@ class CacheDesc(C.Structure):
 class TablesDesc(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in
                 ("held", "fresh", "parent", "pages_held", "free_pages", "n_free", "page_table", "pages_held_out", "n_free_out",
-                 "seq_lens", "first", "seq_id", "pos", "slot", "tree_mask", "result")]
+                 "seq_lens", "first", "seq_id", "pos", "slot", "tree_mask", "result", "granted")]
 
 
 _lib = None
@@ -294,7 +294,8 @@ def elitekv_attend_rows(layer: Layer, cache: CacheDesc, q_rope, q_abs, seq_lens,
 
 class Tables:
     """Inputs (the caller's tensors) and outputs (made here, or given as `outputs`) of elitekv_step_tables; serves step
-    after step.  result is int32 [4] on the device: status, new tokens, pages taken, detail."""
+    after step.  result is int32 [4] on the device: status, new tokens, pages taken, detail; granted int32 [B] is what the attention
+    and the acceptance take as n_nodes (fresh, or 0 in a refused step)."""
 
     def __init__(self, B, n_slots, m, inputs, outputs):
         self.B, self.n_slots, self.m = B, n_slots, m
@@ -329,7 +330,7 @@ def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_
     outputs = {"page_table": page_table, "pages_held_out": empty(B) if paged else None, "n_free_out": empty(1) if paged else None,
                "seq_lens": empty(B), "first": empty(B + 1), "seq_id": empty(n_slots), "pos": empty(n_slots),
                "slot": empty(n_slots, dtype=torch.int64), "tree_mask": empty(B, m, dtype=torch.int64) if m > 0 else None,
-               "result": empty(4)}
+               "result": empty(4), "granted": empty(B)}
     return Tables(B, n_slots, m, inputs, outputs)
 
 

@@ -162,6 +162,7 @@ step_tables_kernel(const TabArgs a) {
     const int held = t.held[b];
     t.seq_lens[b] = ok ? held + t.fresh[b] : held;
     t.first[b] = ok ? s_tok[b] : 0;
+    if (t.granted) t.granted[b] = ok ? t.fresh[b] : 0;
     if (paged) t.pages_held_out[b] = t.pages_held[b] + (ok ? s_pg[b + 1] - s_pg[b] : 0);
   }
   if (g0 == 0) {
@@ -242,7 +243,7 @@ extern "C" int elitekv_step_tables(const elitekv_cache* cache, const elitekv_tab
   if (m > 0 ? n_slots != (int64_t)B * m || !t.tree_mask : t.parent != nullptr) return ELITEKV_ERR_INVALID_ARG;
   if (((uintptr_t)t.slot & 7) || ((uintptr_t)t.tree_mask & 7)) return ELITEKV_ERR_INVALID_ARG;
   // inputs that every block reads are not written by any
-  if (t.seq_lens == t.held || t.seq_lens == t.fresh) return ELITEKV_ERR_INVALID_ARG;
+  if (t.seq_lens == t.held || t.seq_lens == t.fresh || (t.granted && (t.granted == t.held || t.granted == t.fresh))) return ELITEKV_ERR_INVALID_ARG;
   TabArgs a;
   a.t = t;
   int rc = ekv_make_view(cache, &a.cv);
