@@ -287,7 +287,7 @@ int elitekv_append_slots(const elitekv_layer* layer, const elitekv_cache* cache,
  * over the tokens that node i sees: all committed ones, t < seq_lens[b] - n_nodes[b], and node j's,
  * t = seq_lens[b] - n_nodes[b] + j, where bit j of tree_mask[b][i] is set.  A row that sees nothing,
  * and every row i >= n_nodes[b], is a zero row.  Tokens that a row does not see do not touch it,
- * whatever their cache rows hold.
+ * whatever their cache rows hold, and a rope value that is not finite touches its own head only.
  *   q_rope bf16 [B][m][n_h][2r], q_abs bf16 [B][m][n_h][d_c] (separated latents: d_ck), 16-byte aligned
  *   seq_lens int32 [B] cached tokens, nodes included; n_nodes int32 [B] in [0, m], NULL: m everywhere
  *   tree_mask uint64 [B][m];   out bf16 [B][m][n_h][d_h], 4-byte aligned

@@ -31,6 +31,11 @@
 // results do not depend on scheduling, and the partial results' number does not grow with the context.  Runs are cut by the
 // prep kernel, on the device, where the lengths are.
 //
+// A rope value that is not finite is its head's matter alone, but in the score product it meets the zeros of the other heads in its
+// row block, and 0 times it is NaN.  So a block whose scores hold NaN looks at them one by one, and those of tokens with
+// such values among the row block's rope columns are computed again on FP32 lanes from the row's own head.  A call without
+// such values pays a look at the sums (0 to 0.6 %); 13B, 8 x 8192 tokens that all hold them, 32 nodes: 236 ms.
+//
 // Tokens that a row does not see: their scores are dropped by a select, P = 0.  In the value product 0 times a value that
 // is not finite would spread it to every row, so the drafted tokens' rows (and the rest of the last 64 tokens) pass a
 // warp that clears such values before the tensor core reads them, and notes the nodes: rows that see one become NaN.
@@ -84,9 +89,10 @@ struct TreeQueryMaps {
 
 struct TreeTcArgs {
   CacheView cv;
+  const bf16 *q_rope, *q_abs, *rope, *latent;      // (for scores that are computed again)
   const uint64_t* mask;
   TreeLayouts lay;
-  int m, n_h, r2, kw, vw, n_rb, n_ct, box_s, box_v, v3;       // n_rb: of the first layout
+  int m, n_h, r2, kw, vw, d_c, n_rb, n_ct, box_s, box_v, v3;       // n_rb: of the first layout
   float scale_log2e;
   bf16* P;                    // [slot][CG][kPiece / 64][128][64]: what a step loads is one piece (4 KB from row to row: 655 clocks a
                               // step instead of 530)
@@ -160,6 +166,24 @@ __device__ __forceinline__ long long tree_row(const CacheView& cv, int b, int t,
   return ((long long)page << cv.page_shift) + (t & cv.page_mask);
 }
 
+// Whether one of eight bf16 values is not finite, and their product with eight others added to s
+__device__ __forceinline__ bool any_not_finite(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
+__device__ __forceinline__ float dot8(const uint4& x, const uint4& y, float s) {
+  const uint32_t v[4] = {x.x, x.y, x.z, x.w}, w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    s = fmaf(__uint_as_float(v[e] << 16), __uint_as_float(w[e] << 16), s);
+    s = fmaf(__uint_as_float(v[e] & 0xffff0000u), __uint_as_float(w[e] & 0xffff0000u), s);
+  }
+  return s;
+}
+
 // first rope column that a row block's score product takes: of its first head, on a 16-byte boundary
 __host__ __device__ __forceinline__ int tree_rope_col(int h0, int r2) { return h0 * r2 & ~7; }
 
@@ -188,12 +212,46 @@ __device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int
 }
 __device__ __forceinline__ int walk_len(const PieceWalk& w) { return min(kPiece, w.r.z - w.k * kPiece); }
 
+// A warp's scores of tokens t0 .. t0 + tokens - 1 that are NaN for another head's rope values (columns [x0, x0 + cols) are
+// the row block's): computed again, into the tile.  Whether there was one.  (A function of its own: inline it cost the kernel 80
+// bytes of spilled registers.)
+__device__ __noinline__ bool mend_scores(const TreeTcArgs& a, uint32_t tm, int b, int h, int i, int t0, int tokens, int prefix,
+                                         unsigned long long mask, bool active, int x0, int cols) {
+  const int lane = threadIdx.x & 31;
+  const long long row = ((long long)b * a.m + i) * a.n_h + h;
+  bool any = false;
+#pragma unroll 1
+  for (int t = 0; t < tokens; ++t) {
+    float v = tc_ld1(tm + t);
+    tc_wait_ld();
+    const int node = t0 + t - prefix;
+    const bool want = active && v != v && (node < 0 || (mask >> node & 1));
+    if (!__any_sync(0xffffffffu, want)) continue;
+    const long long at = tree_row(a.cv, b, t0 + t, nullptr);
+    const bf16* const kr = a.rope + at * a.n_h * a.r2;
+    bool bad = false;
+    for (int k = lane * 8; k < cols; k += 256) bad |= any_not_finite(__ldcg((const uint4*)(kr + x0 + k)));
+    if (!__any_sync(0xffffffffu, bad)) continue;           // (the latents or the query make them so)
+    if (want) {
+      const bf16 *const c = a.latent + at * a.d_c, *const q = a.q_abs + row * a.kw;
+      v = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < a.kw; k += 8) v = dot8(__ldcg((const uint4*)(q + k)), __ldcg((const uint4*)(c + k)), v);
+      for (int k = 0; k < a.r2; ++k) v = fmaf(__bfloat162float(a.q_rope[row * a.r2 + k]), __bfloat162float(kr[h * a.r2 + k]), v);
+    }
+    tc_st1(tm + t, v);
+    tc_wait_st();
+    any = true;
+  }
+  return any;
+}
+
 template <int CG>
 __global__ void __launch_bounds__(kTreeThreads, 1)
 tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_p,
                const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ CUtensorMap map_r,
-               const __grid_constant__ CUtensorMap map_ps, const __grid_constant__ CUtensorMap map_o, const TreeTcArgs a) {
+               const __grid_constant__ CUtensorMap map_ps, const __grid_constant__ CUtensorMap map_o, const __grid_constant__ TreeTcArgs a) {
   using SM = TreeSmem<CG>;
   constexpr int NST = SM::n_stages;
   extern __shared__ unsigned char smem_raw[];
@@ -669,7 +727,7 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
         };
         // one pass with the reference 0; another where a row's largest score is out of range
         float ref = 0.f, sum = 0.f;
-        for (bool again = false;;) {
+        for (bool again = false, looked = a.lay.of[lay].n_rc == 0;;) {
           float top = -INFINITY, sum4[4] = {0.f, 0.f, 0.f, 0.f};
           auto chunk = [&](int cc, float* x) {                     // 32 tokens
             if (!all) {
@@ -716,6 +774,15 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
           }
           sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
           if (again) break;
+          if (!looked && __any_sync(0xffffffffu, active && sum != sum)) {
+            looked = true;
+            const int x0 = tree_rope_col(rb * CG * hb, a.r2), cols = min(a.lay.of[lay].n_rc * 64, a.n_h * a.r2 - x0);
+            if (mend_scores(a, tm, b, h, i, t0, min(kTile, n - t0), prefix, active ? mask : 0ull, active, x0, cols)) {
+              if (lane == 0) bulk_wait_group_all();
+              __syncwarp();
+              continue;
+            }
+          }
           // (rows of padding nodes weigh nothing, whatever their queries hold)
           top *= a.scale_log2e;
           ref = !active || top == -INFINITY || fabsf(top) <= 64.f ? 0.f : 64.f * rintf(top * (1.f / 64.f));
@@ -1546,8 +1613,13 @@ int ekv_launch_tree_tc(const elitekv_layer* L, const elitekv_cache* cache, const
   const int page = cv.page_table ? 1 << cv.page_shift : 1 << 30;
   TreeTcArgs a;
   a.cv = cv;
+  a.q_rope = (const bf16*)c.q_rope;
+  a.q_abs = (const bf16*)c.q_abs;
+  a.rope = (const bf16*)cache->rope;
+  a.latent = (const bf16*)cache->latent;
   a.mask = c.mask;
   a.m = c.m;
+  a.d_c = L->d_c;
   a.n_h = L->n_h;
   a.r2 = 2 * L->r;
   a.kw = L->kw;
