@@ -43,6 +43,7 @@
 // Every wait is bounded; when one runs out the block records ELITEKV_ERR_TIMEOUT and leaves.
 #include "tc_ptx.cuh"
 #include "tree.cuh"
+#include "tree_steps.cuh"
 
 namespace {
 
@@ -332,7 +333,7 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
       if (lane == 0) release_unit();
       if (type == kStop) break;
       if (type == kScore) {
-        const int all = min(kTile / a.box_s, (n - (tok0 + idx * kTile) + a.box_s - 1) / a.box_s);      // boxes of tokens, both blocks
+        const int all = tree_score_boxes_all(n - (tok0 + idx * kTile), kTile, a.box_s, CG);      // boxes of tokens, both blocks
         const TreeLayout& l = a.lay.of[lay];
         const CUtensorMap* const map_q = &maps_q.of[lay];
         const int h0 = (rb * CG + (int)rank) * l.hb, nkc = nkl + l.n_rc;
@@ -361,7 +362,7 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
       } else {
         fence_proxy_all();                  // (P of the piece is complete: the unit was published after that)
         const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
-        const int ch_all = a.v3 ? kTile / 64 : min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);      // 64-column chunks loaded, both blocks
+        const int ch_all = a.v3 ? kTile / 64 : tree_value_chunks_all(min(kTile / 64, (a.vw - idx * kTile + 63) >> 6), CG);      // 64-column chunks loaded, both blocks
         const int y = (slot * CG + (int)rank) * (kPiece / 64) * kRows;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int t0 = tok0 + ks * 64, boxes = min(per, (n - t0 + bv - 1) / bv);
@@ -383,7 +384,7 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
       if (!ok) break;
     }
   } else if (warp == 2) {
-    // ============================================================== cache rows
+    // ============================================================== cache rows (a box at least in every step: csrc/tree_steps.cuh)
     // Where either product reads a cache row once (one row block), the rows give way in L2 to what is read again: queries, P,
     // partial results (16 x 4096 tokens of 7B, 4 nodes: 134.5 -> 127.7 us, 16 x 2000: 107 -> 95; keeping some of the rows from
     // the score product to the value product by priority was slower, whatever their number)
@@ -401,9 +402,9 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
       if (type == kStop) break;
       if (type == kScore) {
         const int t0 = tok0 + idx * kTile + (int)rank * (kTile / CG);
-        const int bs = a.box_s, mine = min(kTile / CG / bs, max(0, (n - t0 + bs - 1) / bs));      // boxes; lane j knows box j's rows
-        int row = 0;
-        if (lane < mine) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
+        const int bs = a.box_s, mine = tree_score_boxes(n - t0, kTile / CG, bs);      // boxes; lane j knows box j's rows
+        int row = -bs;                       // (nothing left here: a box before the plane's first row)
+        if (lane < mine && t0 < n) row = (int)tree_row(a.cv, b, t0 + lane * bs, a.status);
         const int xr = tree_rope_col(rb * CG * a.lay.of[lay].hb, a.r2), nkc = nkl + a.lay.of[lay].n_rc;
         for (int kc = 0; kc < nkc; ++kc, ++pos) {
           const unsigned st = pos % NST;
@@ -425,8 +426,8 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
       } else {
         const int bv = a.box_v, per = 64 / bv, ks_n = (len + 63) >> 6;
         // this block's columns: its half of the tile's (a quarter where half of the tile is enough: the product's width is halved)
-        const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6), mine = ch_all <= 2 ? 2 / CG : 4 / CG;
-        const int x0 = idx * kTile + (int)rank * mine * 64, ch = a.v3 ? 4 / CG : max(0, min(mine, ch_all - mine * (int)rank));
+        const int held = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6), mine = tree_value_share(held, CG);
+        const int x0 = idx * kTile + (int)rank * mine * 64, ch = a.v3 ? 4 / CG : tree_value_chunks(held, CG, (int)rank);
         int row = 0;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int b0 = ks * per;                    // first box of the step
@@ -534,8 +535,8 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
         pos += nkl + a.lay.of[lay].n_rc;
       } else {
         const int ks_n = (len + 63) >> 6;
-        const int ch_all = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
-        const int mine = ch_all <= 2 ? 2 / CG : 4 / CG, ch = max(0, min(mine, ch_all - mine * (int)rank));      // (chunks past the last column are not stored)
+        const int held = min(kTile / 64, (a.vw - idx * kTile + 63) >> 6);
+        const int ch = max(0, min(tree_value_share(held, CG), held - tree_value_share(held, CG) * (int)rank));      // (chunks past the last column are not stored)
         unsigned nf_lo = 0, nf_hi = 0;
         for (int ks = 0; ks < ks_n; ++ks, ++pos) {
           const int t0 = tok0 + ks * 64;
