@@ -311,13 +311,12 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
   unsigned q_pos = 0;
   auto q_slot = [&]() { return q_pos % kQueue; };
   auto q_parity = [&]() { return (q_pos / kQueue) & 1u; };
-  // Arrival on a barrier of the first block that only says "read": what it stands for (words of shared memory, tensor memory
-  // that tcgen05.wait::ld has waited for) is in registers.  (With release semantics over the cluster it held the warp
-  // that issues the products for 2500 clocks a unit.)
-  auto arrive_read = [&](uint32_t bar) {             // one lane of a warp
-    if (rank == 0) mbar_arrive(bar); else mbar_arrive_cluster_relaxed(map_to_cta(bar, 0));
+  // A unit's words given back (one lane of a warp).  The release orders the warp's reads of them before the other block's warp
+  // writes the next unit there (1 % of the long cases; a relaxed arrival would order nothing).
+  auto release_unit = [&]() {
+    const uint32_t bar = smem_u32(&bars->q_empty[q_slot()]);
+    if (rank == 0) mbar_arrive(bar); else mbar_arrive_cluster(map_to_cta(bar, 0));
   };
-  auto release_unit = [&]() { arrive_read(smem_u32(&bars->q_empty[q_slot()])); };
 
   if (warp == 0) {
     // ============================================================== queries, P (and the bytes that a step expects)
@@ -709,7 +708,12 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
       auto acc_done = [&]() {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_read(smem_u32(&bars->acc_empty[group_id]));
+        // What the arrival stands for is in registers: tcgen05.wait::ld has waited for it.  (With release semantics over the
+        // cluster it held the warp that issues the products for 2500 clocks a unit.)
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&bars->acc_empty[group_id]);
+          if (rank == 0) mbar_arrive(bar); else mbar_arrive_cluster_relaxed(map_to_cta(bar, 0));
+        }
       };
       if (type == kScore) {
         const int t0 = tok0 + idx * kTile;
