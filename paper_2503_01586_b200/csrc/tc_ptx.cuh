@@ -281,15 +281,6 @@ __device__ __forceinline__ void tc_ld8(uint32_t taddr, float* v) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr) : "memory");
 }
-// one column: a value per lane
-__device__ __forceinline__ float tc_ld1(uint32_t taddr) {
-  uint32_t r;
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
-  return __uint_as_float(r);
-}
-__device__ __forceinline__ void tc_st1(uint32_t taddr, float v) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%1], {%0};" ::"r"(__float_as_uint(v)), "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void tc_st8(uint32_t taddr, const float* v) {
   const uint32_t* r = (const uint32_t*)v;
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"

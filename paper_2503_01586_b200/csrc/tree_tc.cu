@@ -34,7 +34,7 @@
 // A rope value that is not finite is its head's matter alone, but in the score product it meets the zeros of the other heads in its
 // row block, and 0 times it is NaN.  So a block whose scores hold NaN looks at them one by one, and those of tokens with
 // such values among the row block's rope columns are computed again on FP32 lanes from the row's own head.  A call without
-// such values pays a look at the sums (0 to 0.6 %); 13B, 8 x 8192 tokens that all hold them, 32 nodes: 236 ms.
+// such values pays a look at the sums (0 to 0.6 %); 13B, 8 x 8192 tokens that all hold them, 32 nodes: 71 ms.
 //
 // Tokens that a row does not see: their scores are dropped by a select, P = 0.  In the value product 0 times a value that
 // is not finite would spread it to every row, so the drafted tokens' rows (and the rest of the last 64 tokens) pass a
@@ -148,8 +148,9 @@ __device__ __forceinline__ bool poll_global(const int* p, int target, volatile i
   if (*abort_flag == 0) *abort_flag = why;
   return false;
 }
+// (the limit is some 0.6 s or more: a tile whose scores are all computed again takes milliseconds, and a wait may span several)
 __device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, int why) {
-  for (unsigned i = 0; i < kWaitLimit; ++i) {
+  for (unsigned i = 0; i < kSpinLimit; ++i) {
     if (__any_sync(0xffffffffu, mbar_try_wait_cluster(bar, parity))) return true;
     if ((i & 1023) == 1023 && __any_sync(0xffffffffu, *abort_flag != 0)) return false;
   }
@@ -214,35 +215,59 @@ __device__ __forceinline__ void walk_next(PieceWalk& w, const TreeTcArgs& a, int
 __device__ __forceinline__ int walk_len(const PieceWalk& w) { return min(kPiece, w.r.z - w.k * kPiece); }
 
 // A warp's scores of tokens t0 .. t0 + tokens - 1 that are NaN for another head's rope values (columns [x0, x0 + cols) are
-// the row block's): computed again, into the tile.  Whether there was one.  (A function of its own: inline it cost the kernel 80
-// bytes of spilled registers.)
+// the row block's): computed again, into the tile.  Whether there was one.  Eight tokens at a time share a lane's read of its query
+// (13B, 8 x 8192 tokens that all need it, 32 nodes: 71 ms; one at a time 236).  (A function of its own: inline it cost the kernel 80 bytes of spilled registers.)
 __device__ __noinline__ bool mend_scores(const TreeTcArgs& a, uint32_t tm, int b, int h, int i, int t0, int tokens, int prefix,
                                          unsigned long long mask, bool active, int x0, int cols) {
+  constexpr int kMend = 8;
   const int lane = threadIdx.x & 31;
   const long long row = ((long long)b * a.m + i) * a.n_h + h;
   bool any = false;
 #pragma unroll 1
-  for (int t = 0; t < tokens; ++t) {
-    float v = tc_ld1(tm + t);
+  for (int t = 0; t < tokens; t += kMend) {
+    float v[kMend], s[kMend];
+    int at[kMend];                         // cache rows (box coordinates: below 2^31)
+    unsigned redo = 0, mine = 0;           // tokens to compute again: of any lane, of this one
+    tc_ld8(tm + t, v);
     tc_wait_ld();
-    const int node = t0 + t - prefix;
-    const bool want = active && v != v && (node < 0 || (mask >> node & 1));
-    if (!__any_sync(0xffffffffu, want)) continue;
-    const long long at = tree_row(a.cv, b, t0 + t, nullptr);
-    const bf16* const kr = a.rope + at * a.n_h * a.r2;
-    bool bad = false;
-    for (int k = lane * 8; k < cols; k += 256) bad |= any_not_finite(__ldcg((const uint4*)(kr + x0 + k)));
-    if (!__any_sync(0xffffffffu, bad)) continue;           // (the latents or the query make them so)
-    if (want) {
-      const bf16 *const c = a.latent + at * a.d_c, *const q = a.q_abs + row * a.kw;
-      v = 0.f;
-#pragma unroll 4
-      for (int k = 0; k < a.kw; k += 8) v = dot8(__ldcg((const uint4*)(q + k)), __ldcg((const uint4*)(c + k)), v);
-      for (int k = 0; k < a.r2; ++k) v = fmaf(__bfloat162float(a.q_rope[row * a.r2 + k]), __bfloat162float(kr[h * a.r2 + k]), v);
+#pragma unroll
+    for (int e = 0; e < kMend; ++e) {
+      const int node = t0 + t + e - prefix;
+      const bool want = active && v[e] != v[e] && t + e < tokens && (node < 0 || (mask >> node & 1));
+      s[e] = 0.f;
+      at[e] = 0;
+      if (!__any_sync(0xffffffffu, want)) continue;
+      at[e] = (int)tree_row(a.cv, b, t0 + t + e, nullptr);
+      bool bad = false;
+      for (int k = lane * 8; k < cols; k += 256) bad |= any_not_finite(__ldcg((const uint4*)(a.rope + (long long)at[e] * a.n_h * a.r2 + x0 + k)));
+      if (!__any_sync(0xffffffffu, bad)) continue;           // (the latents or the query make them so)
+      redo |= 1u << e;
+      if (want) mine |= 1u << e;
     }
-    tc_st1(tm + t, v);
-    tc_wait_st();
+    if (redo == 0) continue;
     any = true;
+    if (mine != 0) {
+      const bf16 *const q = a.q_abs + row * a.kw, *const qr = a.q_rope + row * a.r2;
+#pragma unroll 2
+      for (int k = 0; k < a.kw; k += 8) {
+        const uint4 x = __ldcg((const uint4*)(q + k));
+        uint4 y[kMend];                    // (tokens that need none take row 0: a branch would make the loads wait for one another)
+#pragma unroll
+        for (int e = 0; e < kMend; ++e) y[e] = __ldcg((const uint4*)(a.latent + (long long)at[e] * a.d_c + k));
+#pragma unroll
+        for (int e = 0; e < kMend; ++e) s[e] = dot8(x, y[e], s[e]);
+      }
+      for (int k = 0; k < a.r2; ++k) {
+        const float x = __bfloat162float(qr[k]);
+#pragma unroll
+        for (int e = 0; e < kMend; ++e) s[e] = fmaf(x, __bfloat162float(a.rope[((long long)at[e] * a.n_h + h) * a.r2 + k]), s[e]);
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < kMend; ++e) v[e] = mine >> e & 1 ? s[e] : v[e];
+    tc_st8(tm + t, v);
+    tc_wait_st();
   }
   return any;
 }
@@ -679,7 +704,7 @@ tree_tc_kernel(const __grid_constant__ TreeQueryMaps maps_q, const __grid_consta
     };
     auto group_bar = [&](uint32_t bar, uint32_t parity, int why) -> bool {
       const bool ok = group([&]() {
-        for (unsigned k = 0; k < kWaitLimit; ++k) {
+        for (unsigned k = 0; k < kSpinLimit; ++k) {
           if (mbar_try_wait_cluster(bar, parity)) return true;
           if ((k & 1023) == 1023 && *s_abort) return false;
         }

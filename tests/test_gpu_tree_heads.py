@@ -71,3 +71,16 @@ def test_a_cache_of_them(ek):
     check_tree(s, out, [0, 1])
     for b, k in enumerate(nodes):
         assert out[b, :k, 2:].isnan().all()
+
+
+@pytest.mark.parametrize("n_h,d_c,lens,m", [(32, 4096, [1100, 700], 32), (16, 8192, [2048, 300], 64)])
+def test_wide_latents_and_a_cache_of_them(ek, n_h, d_c, lens, m):
+    """Where every score of a tile is computed again over thousands of latents, the waits of the others are long, but run out
+    nowhere."""
+    w = replace(gen.TINY, n_h=n_h, d_h=128, r=8, d_c=d_c, d=n_h * 128)
+    s = tree_state(ek, w, lens, [m, m], m, seed=7)
+    for b in range(2):
+        s["rope"][s["where"][b], 2 * 2 * w.r:] = NAN
+    out = call_tree(ek, s)
+    check_tree(s, out, [1], seqs=[1])
+    assert out[:, :, :2].isfinite().all() and out[:, :, 2:].isnan().all()
