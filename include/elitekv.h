@@ -239,7 +239,7 @@ typedef struct {
   const int32_t* parent;       /* [B][m], or NULL: a chain                                            */
   const int32_t* pages_held;   /* [B] valid entries of the sequence's row of the page table, at least
                                   ceil(held / page_size)                                              */
-  const int32_t* free_pages;   /* [n_free] stack of free page ids, its top at the end                 */
+  const int32_t* free_pages;   /* [n_free] stack of free page ids, its top at the end; NULL: empty    */
   const int32_t* n_free;       /* [1]                                                                 */
   /* out */
   int32_t* page_table;         /* the cache's own page table                                          */
@@ -267,7 +267,8 @@ typedef struct {
  *   ELITEKV_ERR_NO_PAGES      result[3] pages are missing
  *   ELITEKV_ERR_BAD_POSITION  sequence result[3]: negative lengths, more tokens than the cache holds, more
  *                             than m, fewer pages held than tokens; or -1: more tokens than n_slots
- *   ELITEKV_ERR_BAD_PAGE      result[3]: a page id outside the pool, among those the new tokens go to
+ *   ELITEKV_ERR_BAD_PAGE      result[3]: a page id outside the pool, among those the new tokens go to, or an n_free
+ *                             that is none of a stack of the pool's pages
  * and then nothing is granted: the page table is as it was, every entry is padding, seq_lens = held,
  * first = 0, granted = 0, pages_held_out = pages_held, n_free_out = n_free.
  * B <= ELITEKV_MAX_TABLE_SEQS, sequences 0 .. B-1 of the cache. */
