@@ -293,7 +293,9 @@ int elitekv_append_slots(const elitekv_layer* layer, const elitekv_cache* cache,
  *   seq_lens int32 [B] cached tokens, nodes included; n_nodes int32 [B] in [0, m], NULL: m everywhere
  *   tree_mask uint64 [B][m];   out bf16 [B][m][n_h][d_h], 4-byte aligned
  *   workspace: 256-byte aligned, elitekv_attend_tree_workspace_size bytes (of shape, B, m and device, not
- *   of the lengths), private to this call until the stream reaches its end.
+ *   of the lengths; enough for every call of fewer sequences and nodes too), private to this call until the
+ *   stream reaches its end.  Partial results in fp32 are most of it: 64 sequences of 64 nodes take 1.6 GB with
+ *   32 heads and 1536 latents, 2.5 GB with 40 and 1920; one sequence 90 to 110 MB.
  * 1 <= m <= ELITEKV_MAX_TREE_NODES; any layer and page size.  Results do not depend on scheduling.
  * A length outside the cache and a node count outside [0, m] or above the length are recorded (BAD_POSITION,
  * detail = sequence, length) and clamped, a page id outside the pool (BAD_PAGE) counts as page 0. */

@@ -209,12 +209,13 @@ struct GenCarve {
   size_t first, ml, acc, slice, cnt, total;
 };
 GenCarve generic_carve(const elitekv_layer* L, int B, int m) {
-  const size_t items = (size_t)B * generic_splits(L, B, m), rows = (size_t)m * L->n_h;
+  // (rows x splits is at most this, which grows with B and m as the splits, rounded, do not)
+  const size_t rows = (size_t)B * m * L->n_h, most = rows + 16 * (size_t)L->sm_count, parts = rows * kSplits < most ? rows * kSplits : most;
   GenCarve c;
   size_t o = 0;
   c.first = o; o = align256(o + sizeof(int32_t) * ((size_t)B + 1));
-  c.ml = o;    o = align256(o + sizeof(float) * 2 * items * rows);
-  c.acc = o;   o = align256(o + sizeof(float) * items * rows * L->vw);
+  c.ml = o;    o = align256(o + sizeof(float) * 2 * parts);
+  c.acc = o;   o = align256(o + sizeof(float) * parts * L->vw);
   c.slice = o; o = align256(o + ekv_combine_scratch_bytes(L, B) * m);
   c.cnt = o;   o = align256(o + sizeof(int32_t) * (size_t)ekv_combine_counters(L, B) * m);
   c.total = o;
@@ -275,15 +276,29 @@ int ekv_launch_tree_generic(const elitekv_layer* L, const elitekv_cache* cache, 
   return ekv_launch_combine(L, c.B, ws, c.out, st);
 }
 
-extern "C" int elitekv_attend_tree_workspace_size(const elitekv_layer* L, int32_t B, int32_t m, size_t* bytes) {
-  if (!L || !bytes || B <= 0 || m < 1 || m > ELITEKV_MAX_TREE_NODES) return ELITEKV_ERR_INVALID_ARG;
-  // the cache's layout is not known here: enough for either kernel
+namespace {
+
+// What a call of this size uses, whatever kernel the cache's layout leads to
+size_t tree_need(const elitekv_layer* L, int B, int m) {
   const size_t g = ekv_tree_generic_bytes(L, B, m), t = ekv_tree_tc_supported(L, B, m, nullptr) ? ekv_tree_tc_bytes(L, B, m) : 0;
   const size_t r = ekv_tree_rows_bytes(L, B, m);
-  *bytes = g > t ? g : t;
-  if (r > *bytes) *bytes = r;
-  size_t d = 0;
-  if (m == 1 && elitekv_decode_workspace_size(L, B, &d) == ELITEKV_OK && d + lens_bytes(B) > *bytes) *bytes = d + lens_bytes(B);
+  size_t most = g > t ? g : t, d = 0;
+  if (r > most) most = r;
+  if (m == 1 && elitekv_decode_workspace_size(L, B, &d) == ELITEKV_OK && d + lens_bytes(B) > most) most = d + lens_bytes(B);
+  return most;
+}
+
+}  // namespace
+
+// Fewer nodes may need more (fewer row blocks are cut into more runs, another kernel serves them): the size is that of the
+// largest tree and of all smaller ones.
+extern "C" int elitekv_attend_tree_workspace_size(const elitekv_layer* L, int32_t B, int32_t m, size_t* bytes) {
+  if (!L || !bytes || B <= 0 || m < 1 || m > ELITEKV_MAX_TREE_NODES) return ELITEKV_ERR_INVALID_ARG;
+  *bytes = 0;
+  for (int k = 1; k <= m; ++k) {
+    const size_t n = tree_need(L, B, k);
+    if (n > *bytes) *bytes = n;
+  }
   return ELITEKV_OK;
 }
 
@@ -297,10 +312,7 @@ extern "C" int elitekv_attend_tree(const elitekv_layer* L, const elitekv_cache* 
   CacheView cv;
   int rc = ekv_make_view(cache, &cv);
   if (rc != ELITEKV_OK) return rc;
-  size_t need = 0;
-  rc = elitekv_attend_tree_workspace_size(L, B, m, &need);
-  if (rc != ELITEKV_OK) return rc;
-  if (((uintptr_t)workspace & 255) || workspace_bytes < need) return ELITEKV_ERR_WORKSPACE_TOO_SMALL;
+  if (((uintptr_t)workspace & 255) || workspace_bytes < tree_need(L, B, m)) return ELITEKV_ERR_WORKSPACE_TOO_SMALL;
   const TreeCall c{q_rope, q_abs, seq_lens, n_nodes, tree_mask, B, m, workspace, out};
   const bool dense = ekv_tree_tc_supported(L, B, m, &cv) != 0;
   int32_t plan[5];
