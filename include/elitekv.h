@@ -230,7 +230,7 @@ int elitekv_attend_rows(const elitekv_layer* layer, const elitekv_cache* cache, 
 #define ELITEKV_MAX_TREE_NODES 64
 #define ELITEKV_MAX_TABLE_SEQS 8192
 
-/* Inputs and outputs of elitekv_step_tables.  Host struct, DEVICE pointers; outputs overlap no
+/* Inputs and outputs of elitekv_step_tables.  Host struct, DEVICE pointers (of the current device); outputs overlap no
  * input, except that page_table is updated in place (entries of pages already held are not written). */
 typedef struct {
   /* in */

@@ -306,6 +306,7 @@ class Tables:
         for k, v in outputs.items():
             setattr(self, k, v)
         self.desc = desc
+        self.device = inputs["held"].device.index
 
 
 def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_table=None, pages_held=None, free_pages=None,
@@ -317,6 +318,8 @@ def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_
     for v in [*inputs.values(), page_table]:
         if v is not None:
             _dev(v, i32)
+    if any(v.device != dev for v in [*inputs.values(), page_table] if v is not None):
+        raise ValueError("make_tables: all tensors are on one device")
     if held.numel() < B or fresh.numel() < B:
         raise ValueError("make_tables: held and fresh have an entry per sequence")
     if m > 0 and (n_slots != B * m or (parent is not None and parent.numel() < B * m)):
@@ -335,7 +338,12 @@ def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_
 
 
 def elitekv_step_tables(cache: CacheDesc, tables: Tables) -> Tables:
-    _check(lib().elitekv_step_tables(C.byref(cache), C.byref(tables.desc), tables.B, tables.m, tables.n_slots, _stream()),
+    # no layer here that the library could compare the current device with
+    device = torch.cuda.current_device()
+    if tables.device != device:
+        raise ValueError("elitekv_step_tables: the tables are on another device than the current one")
+    stream = _raw_stream(device) if _raw_stream is not None else _stream()
+    _check(lib().elitekv_step_tables(C.byref(cache), C.byref(tables.desc), tables.B, tables.m, tables.n_slots, stream),
            "elitekv_step_tables")
     return tables
 

@@ -1,0 +1,38 @@
+"""The binding keeps the tables' tensors on one device, the current one (no GPU: stand-ins for tensors)."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2503_01586_b200 import binding as ek
+
+
+class OnDevice:
+    """What make_tables asks of a tensor before it makes the outputs."""
+    is_cuda, dtype = True, torch.int32
+
+    def __init__(self, index, n=8):
+        self.device, self.n = torch.device("cuda", index), n
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.n
+
+
+@pytest.mark.parametrize("other", ["fresh", "parent", "page_table", "pages_held", "free_pages", "n_free"])
+def test_tensors_of_two_devices_are_refused(other):
+    args = {k: OnDevice(0) for k in ("held", "fresh", "parent", "page_table", "pages_held", "free_pages", "n_free")}
+    args[other] = OnDevice(1)
+    with pytest.raises(ValueError, match="one device"):
+        ek.make_tables(2, 8, 4, **args)
+
+
+def test_tables_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    calls = []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(ek, "lib", lambda: calls.append(1))
+    with pytest.raises(ValueError, match="another device"):
+        ek.elitekv_step_tables(ek.CacheDesc(), SimpleNamespace(device=0, desc=ek.TablesDesc(), B=1, n_slots=1, m=0))
+    assert not calls
