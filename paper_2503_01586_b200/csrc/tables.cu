@@ -66,7 +66,7 @@ step_tables_kernel(const TabArgs a) {
   extern __shared__ int s_tab[];               // first token [B+1], first new page [B+1]
   __shared__ long long s_sum[2][kTabWarps];
   __shared__ int s_bad;
-  __shared__ long long s_page;                  // a bad page id among those that new tokens go to: any int32 may be one
+  __shared__ unsigned s_page;                  // the smallest bad page id among those that new tokens go to, plus 1 (0: a negative one)
   int* const s_tok = s_tab;
   int* const s_pg = s_tab + a.B + 1;
   const elitekv_tables& t = a.t;
@@ -75,7 +75,7 @@ step_tables_kernel(const TabArgs a) {
   const int shift = a.cv.page_shift;
   const long long max_len = paged ? (long long)a.cv.max_pages_per_seq << shift : a.cv.max_ctx;
   constexpr int kNone = 0x7fffffff;             // no sequence
-  constexpr long long kNoPage = 1ll << 32;
+  constexpr unsigned kNoPage = 0xffffffffu;     // (any int32 may be a bad id, the largest as well)
   if (tid == 0) {
     s_bad = kNone;
     s_page = kNoPage;
@@ -103,7 +103,7 @@ step_tables_kernel(const TabArgs a) {
           // pages of the sequence's own that new tokens go to
           for (long long p = held >> shift; p < (end < ph ? end : ph) && fresh > 0; ++p) {
             const int id = t.page_table[(long long)b * a.cv.max_pages_per_seq + p];
-            if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, (long long)(id < 0 ? -1 : id));
+            if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, id < 0 ? 0u : (unsigned)id + 1u);
           }
         }
       }
@@ -146,13 +146,13 @@ step_tables_kernel(const TabArgs a) {
   } else {
     for (int k = tid; k < (int)pg0; k += kTabThreads) {
       const int id = t.free_pages[n_free - 1 - k];
-      if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, (long long)(id < 0 ? -1 : id));
+      if (id < 0 || id >= a.cv.num_pages) atomicMin(&s_page, id < 0 ? 0u : (unsigned)id + 1u);
     }
   }
   __syncthreads();
   if (status == ELITEKV_OK && s_page != kNoPage) {
     status = ELITEKV_ERR_BAD_PAGE;
-    detail = (int)s_page;
+    detail = (int)(s_page - 1u);
   }
   const bool ok = status == ELITEKV_OK;
 
@@ -160,9 +160,10 @@ step_tables_kernel(const TabArgs a) {
   // ---- per sequence and per new page
   for (long long b = g0; b < a.B; b += gs) {
     const int held = t.held[b];
-    t.seq_lens[b] = ok ? held + t.fresh[b] : held;
+    const int fresh = ok ? s_tok[b + 1] - s_tok[b] : 0;
+    t.seq_lens[b] = held + fresh;
     t.first[b] = ok ? s_tok[b] : 0;
-    if (t.granted) t.granted[b] = ok ? t.fresh[b] : 0;
+    if (t.granted) t.granted[b] = fresh;
     if (paged) t.pages_held_out[b] = t.pages_held[b] + (ok ? s_pg[b + 1] - s_pg[b] : 0);
   }
   if (g0 == 0) {
