@@ -371,12 +371,14 @@ def elitekv_attend_tree(layer: Layer, cache: CacheDesc, q_rope, q_abs, seq_lens,
     rows = B * m * layer.n_h
     if q_abs.numel() != rows * layer.kw or (layer.r and q_rope.numel() != rows * 2 * layer.r):
         raise ValueError("elitekv_attend_tree: q_abs is [B][m][n_h][kw], q_rope [B][m][n_h][2r]")
+    if out is not None and out.numel() != rows * layer.d_h:
+        raise ValueError("elitekv_attend_tree: out is [B][m][n_h][d_h]")
     if seq_lens.numel() < B or (n_nodes is not None and n_nodes.numel() < B):
         raise ValueError("elitekv_attend_tree: seq_lens and n_nodes have an entry per sequence")
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("elitekv_attend_tree: the workspace is contiguous CUDA memory")
     if out is None:
         out = torch.empty((B, m, layer.n_h, layer.d_h), dtype=bf16, device=q_abs.device)
-    elif out.numel() != rows * layer.d_h:
-        raise ValueError("elitekv_attend_tree: out is [B][m][n_h][d_h]")
     _check(lib().elitekv_attend_tree(layer.handle, C.byref(cache), None if q_rope is None else _in(q_rope, bf16), _in(q_abs, bf16), _in(seq_lens, i32),
                                      None if n_nodes is None else _in(n_nodes, i32), _in(tree_mask, torch.int64), B, m,
                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _in(out, bf16), _stream()),

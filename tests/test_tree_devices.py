@@ -36,3 +36,14 @@ def test_tables_of_another_device_than_the_current_one_are_refused(monkeypatch):
     with pytest.raises(ValueError, match="another device"):
         ek.elitekv_step_tables(ek.CacheDesc(), SimpleNamespace(device=0, desc=ek.TablesDesc(), B=1, n_slots=1, m=0))
     assert not calls
+
+
+@pytest.mark.parametrize("workspace", [torch.empty(64, dtype=torch.uint8), SimpleNamespace(is_cuda=True, is_contiguous=lambda: False)])
+def test_a_workspace_in_host_memory_or_with_gaps_is_refused(monkeypatch, workspace):
+    """A pointer that the kernels could not read, or bytes that are not one piece."""
+    monkeypatch.setattr(ek, "lib", lambda: pytest.fail("reached the library"))
+    layer, bf16 = SimpleNamespace(handle=None, n_h=2, r=2, d_c=8, d_h=16, kw=8), torch.bfloat16
+    with pytest.raises(ValueError, match="workspace"):
+        ek.elitekv_attend_tree(layer, ek.CacheDesc(), torch.zeros(3, 4, 2, 4, dtype=bf16), torch.zeros(3, 4, 2, 8, dtype=bf16),
+                               torch.zeros(3, dtype=torch.int32), None, torch.zeros(3, 4, dtype=torch.int64), workspace,
+                               torch.zeros(3, 4, 2, 16, dtype=bf16))
