@@ -326,6 +326,8 @@ def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_
         raise ValueError("make_tables: trees have B * m slots and parents")
     if page_table is not None and (pages_held is None or free_pages is None or n_free is None or pages_held.numel() < B):
         raise ValueError("make_tables: a page table comes with pages_held, free_pages and n_free")
+    if page_table is not None and (len(page_table.shape) != 2 or page_table.shape[0] < B or n_free.numel() < 1):
+        raise ValueError("make_tables: the page table has a row per sequence, n_free one entry")
 
     def empty(*shape, dtype=i32):
         return torch.empty(shape, dtype=dtype, device=dev)

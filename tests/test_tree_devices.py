@@ -47,3 +47,11 @@ def test_a_workspace_in_host_memory_or_with_gaps_is_refused(monkeypatch, workspa
         ek.elitekv_attend_tree(layer, ek.CacheDesc(), torch.zeros(3, 4, 2, 4, dtype=bf16), torch.zeros(3, 4, 2, 8, dtype=bf16),
                                torch.zeros(3, dtype=torch.int32), None, torch.zeros(3, 4, dtype=torch.int64), workspace,
                                torch.zeros(3, 4, 2, 16, dtype=bf16))
+
+
+@pytest.mark.parametrize("rows,n_free", [(7, 1), (8, 0)])
+def test_a_page_table_of_too_few_rows_and_a_count_of_no_entries_are_refused(rows, n_free):
+    args = {k: OnDevice(0) for k in ("held", "fresh", "parent", "page_table", "pages_held", "free_pages")} | {"n_free": OnDevice(0, n_free)}
+    args["parent"].n, args["page_table"].shape = 32, (rows, 3)
+    with pytest.raises(ValueError, match="a row per sequence"):
+        ek.make_tables(8, 32, 4, **args)
