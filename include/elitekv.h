@@ -239,7 +239,7 @@ typedef struct {
   const int32_t* parent;       /* [B][m], or NULL: a chain                                            */
   const int32_t* pages_held;   /* [B] valid entries of the sequence's row of the page table, at least
                                   ceil(held / page_size)                                              */
-  const int32_t* free_pages;   /* [n_free] stack of free page ids, its top at the end; NULL: empty    */
+  const int32_t* free_pages;   /* [n_free] stack of free page ids, its top at the end                 */
   const int32_t* n_free;       /* [1]                                                                 */
   /* out */
   int32_t* page_table;         /* the cache's own page table                                          */

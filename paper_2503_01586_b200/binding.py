@@ -329,6 +329,10 @@ def make_tables(B: int, n_slots: int, m: int, held, fresh, *, parent=None, page_
     if page_table is not None and (len(page_table.shape) != 2 or page_table.shape[0] < B or n_free.numel() < 1):
         raise ValueError("make_tables: the page table has a row per sequence, n_free one entry")
 
+    if free_pages is not None and free_pages.numel() == 0:
+        # no page is free: an empty tensor has no address, and the library takes none for a missing argument
+        inputs["free_pages"] = torch.full((1,), -1, dtype=i32, device=dev)
+
     def empty(*shape, dtype=i32):
         return torch.empty(shape, dtype=dtype, device=dev)
     paged = page_table is not None

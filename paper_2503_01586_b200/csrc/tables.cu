@@ -137,7 +137,7 @@ step_tables_kernel(const TabArgs a) {
   } else if (tok0 > 0x7fffffffll || (a.m == 0 && tok0 > a.n_slots)) {
     status = ELITEKV_ERR_BAD_POSITION;
     detail = -1;
-  } else if (paged && (n_free < 0 || n_free > a.cv.num_pages || (n_free > 0 && !t.free_pages))) {
+  } else if (paged && (n_free < 0 || n_free > a.cv.num_pages)) {
     status = ELITEKV_ERR_BAD_PAGE;
     detail = n_free;
   } else if (pg0 > n_free) {
@@ -250,8 +250,8 @@ extern "C" int elitekv_step_tables(const elitekv_cache* cache, const elitekv_tab
   int rc = ekv_make_view(cache, &a.cv);
   if (rc != ELITEKV_OK) return rc;
   if (cache->page_table) {
-    if (!t.page_table || t.page_table != cache->page_table || !t.pages_held || !t.n_free || !t.pages_held_out || !t.n_free_out ||
-        t.pages_held_out == t.pages_held || t.n_free_out == t.n_free)
+    if (!t.page_table || t.page_table != cache->page_table || !t.pages_held || !t.free_pages || !t.n_free || !t.pages_held_out ||
+        !t.n_free_out || t.pages_held_out == t.pages_held || t.n_free_out == t.n_free)
       return ELITEKV_ERR_INVALID_ARG;
   }
   a.B = B;
