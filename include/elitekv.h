@@ -296,7 +296,9 @@ int elitekv_append_slots(const elitekv_layer* layer, const elitekv_cache* cache,
  *   of the lengths; enough for every call of fewer sequences and nodes too), private to this call until the
  *   stream reaches its end.  Partial results in fp32 are most of it: 64 sequences of 64 nodes take 1.6 GB with
  *   32 heads and 1536 latents, 2.5 GB with 40 and 1920; one sequence 90 to 110 MB.
- * 1 <= m <= ELITEKV_MAX_TREE_NODES; any layer and page size.  Results do not depend on scheduling.
+ * 1 <= m <= ELITEKV_MAX_TREE_NODES; any layer and page size.  Results do not depend on scheduling.  Probabilities are
+ * rounded to bf16 for the value product on the tensor cores; the kernel for the smallest calls and for other shapes keeps
+ * them in fp32.  Finite inputs give finite sums for latents below 2^64 / tokens (1e15 for 16384).
  * A length outside the cache and a node count outside [0, m] or above the length are recorded (BAD_POSITION,
  * detail = sequence, length) and clamped, a page id outside the pool (BAD_PAGE) counts as page 0. */
 int elitekv_attend_tree_workspace_size(const elitekv_layer* layer, int32_t B, int32_t m, size_t* bytes);

@@ -257,7 +257,8 @@ extern "C" int elitekv_step_tables(const elitekv_cache* cache, const elitekv_tab
   a.B = B;
   a.m = m;
   a.n_slots = n_slots;
-  // a thread per packed token and a warp per tree, up to a block per SM and a half: every block reads all lengths
+  // a thread per packed token and a warp per tree, up to a fixed cap (no layer here to ask for the device's SMs; 148 on B200):
+  // every block reads all lengths
   const long long want = m > 0 ? (B + kTabWarps - 1) / kTabWarps : (n_slots + kTabThreads - 1) / kTabThreads;
   const unsigned blocks = (unsigned)(want < 1 ? 1 : want > 222 ? 222 : want);
   const size_t smem = sizeof(int) * 2 * ((size_t)B + 1);

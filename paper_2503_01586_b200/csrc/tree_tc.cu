@@ -23,7 +23,7 @@
 //
 // Softmax reference.  P is bf16 and O fp32: both have 8 exponent bits, so the reference of 2^(S - ref) only has to keep
 // the exponents in range.  It is 0 while the largest score of (row, 256 tokens) is within 2^+-64, else a multiple of
-// 64 near it.  All tiles of a row agree on it unless scores are extreme; the block that finishes a piece's last
+// 64 near it (sums over n tokens then stay finite for latents below 2^64 / n).  All tiles of a row agree on it unless scores are extreme; the block that finishes a piece's last
 // score unit looks, and brings P of rows that do not agree to the largest reference: a factor of a power of two, exact.
 // The sums are of the rounded P, so that their rounding cancels where one token dominates.
 //
@@ -1132,7 +1132,7 @@ tree_prep_kernel(const TreePrepArgs a) {
 // ------------------------------------------------------------------ runs joined, W_uv
 // out[b,i,h,:] = (sum over runs 2^(m_run - M) acc_run / L) . W_uv,h: block = (head, as many whole sequences as 128 rows
 // (b, i) hold, a share of the latent axis).  The partial results lie in blocks of 64 latents, in which the m rows of a head
-// are one piece: bulk copies bring (64 latents, one run) of all rows into a ring, eight warps add them up with the runs'
+// are one piece: bulk copies bring (64 latents, one run) of all rows into a ring, kUpWarps warps add them up with the runs'
 // weights and write a bf16 head plus a bf16 remainder as the A tile of two products with W_uv's [64 x d_h] block.  Blocks
 // that share a tile's depth are a cluster; each adds its share of the columns over the others' sums in block order through
 // distributed shared memory.
